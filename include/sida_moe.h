@@ -388,6 +388,96 @@ int sida_hash_forward(const sida_hash_config *cfg, const float *params_dev, cons
 int sida_hash_forward_static(const sida_hash_config *cfg, const float *params_dev, const void *x_dev, int32_t n_seq,
                              int32_t seq_len, int32_t *ids_dev, float *alpha_dev, void *stream);
 
+/* ---- experts in 4 bits: microscaled floating point (MXFP4) -----------------------------------
+ * 32 consecutive values of a row share one power of two s (a byte b stands for 2^(b - 127), b = 255 for NaN), and each
+ * of them is s times a 4-bit value: code c & 7 = 0..7 stands for 0, 0.5, 1, 1.5, 2, 3, 4, 6, and code bit 3 is the sign
+ * (the MX formats of the Open Compute Project, element type E2M1).  An expert matrix takes 17/64 of its bf16 bytes.
+ * No context is needed; the calls are asynchronous on `stream`, allocate nothing and may be captured into a HIP graph.
+ *
+ * Two layouts of a matrix [rows, cols] (cols a multiple of 32; code of column 2i in the low half of byte i of its row):
+ *   SIDA_MX_ROWS   token rows: codes uint8 [rows, cols/2], scales uint8 [rows, 8*ceil(cols/256)] (block i of a row at byte i;
+ *                  bytes past cols/32 are 127 = 2^0).
+ *   SIDA_MX_TILES  expert matrices, in the order in which the matrix cores take them: rows filled up with zeros to a
+ *                  multiple of 32 (R) and columns to one of 64 (C) for the codes and of 256 (C') for the scales, whose
+ *                  filling is 127.
+ *                    codes   16 bytes of row r, columns 32j .. 32j+31, at ((r/32)*(C/32) + j)*512 + (r%32)*16
+ *                    scales  of the same block at ((r/32)*(C'/256) + j/8)*256 + (j%2)*128 + (r%32)*4 + j%8/2
+ *                  Matrices whose row number is a multiple of 32 may follow one another in one call. */
+enum { SIDA_BF16 = 0, SIDA_FP32 = 1, SIDA_MXFP4 = 2 };
+enum { SIDA_MX_ROWS = 0, SIDA_MX_TILES = 1 };
+#define SIDA_MX_MAX_COLS 16384
+/* Bytes of the two arrays of a matrix; 0 on bad arguments (rows < 0, cols not a multiple of 32 in 32 .. SIDA_MX_MAX_COLS). */
+size_t sida_mx_codes_bytes(int64_t rows, int32_t cols, int32_t layout);
+size_t sida_mx_scales_bytes(int64_t rows, int32_t cols, int32_t layout);
+/* Rounds x to MXFP4.  x_dev: SIDA_BF16 or SIDA_FP32 [rows, cols], consecutive rows ld values apart (ld >= cols), at any
+ * address of such a value; on a 16-byte boundary, and with 16-byte multiples between rows, the call is faster.  A block's
+ * power of two is 2^(floor(log2 m) - 2), m its largest magnitude, at least 2^-127 (and 2^-127 where all are 0); values are
+ * divided by it and rounded to the nearest code, ties to the even one, at most 6 in magnitude.  A block that holds an
+ * infinity or a NaN becomes NaN: b = 255, codes 0.
+ * codes_dev (16-byte aligned) and scales_dev (8-byte aligned, in tiles 16): written whole, filling included.  values_dev: NULL, or bf16
+ * [rows, cols], 16-byte aligned: what the codes stand for (exact in bf16), to see or to train through what the rounding changes. */
+int sida_mx_quantize(const void *x_dev, int32_t x_type, int64_t rows, int32_t cols, int64_t ld, int32_t layout,
+                     void *codes_dev, void *scales_dev, void *values_dev, void *stream);
+
+/* Grouped product of token rows with experts in 4 bits: rows offsets[g] .. offsets[g+1]-1 belong to expert g,
+ *     y[r,:] = W_g x[r,:]        (relu != 0: negative results, -0 among them, become 0)
+ * exact products, sums in fp32, one rounding (to nearest even) where y is bf16.  The rows of a sorted batch, as sida_dispatch
+ * leaves them.  One group is a plain product; a single row streams one matrix.
+ *   x_dev       x_type SIDA_BF16: [M, K], rows ldx values apart (ldx >= K), 16-byte aligned, ldx a multiple of 8
+ *               x_type SIDA_MXFP4: codes in SIDA_MX_ROWS layout (16-byte aligned, ldx = K), x_scales_dev their scales (8-byte aligned)
+ *   codes_dev   [groups] matrices [N, K] in SIDA_MX_TILES layout, sida_mx_codes_bytes(N, K, SIDA_MX_TILES) bytes apart (16-byte aligned)
+ *   scales_dev  their scales, likewise (4-byte aligned)
+ *   offsets_dev int32 [groups+1], ascending, 0 .. M.  Values outside are taken as the nearest of 0 and M, a group whose end
+ *               is before its start as empty; rows of y that belong to no group keep what they hold.  NULL with one group: all rows.
+ *   y_dev       y_type SIDA_BF16 or SIDA_FP32: [M, N], rows ldy values apart (ldy >= N), at any address of such a value; where
+ *               rows begin on 16-byte boundaries and N is a multiple of 32, results are stored in whole lines.
+ * Limits: 1 <= groups <= SIDA_MAX_E; K as cols above; 1 <= N <= 65536; 0 <= M <= 2^24; ldx, ldy < 2^24. */
+typedef struct sida_mx_gemm_config {
+    int32_t groups;       /* experts                                       */
+    int32_t N, K;         /* rows and columns of an expert's matrix        */
+    int32_t x_type;       /* SIDA_BF16 or SIDA_MXFP4                       */
+    int32_t y_type;       /* SIDA_BF16 or SIDA_FP32                        */
+    int32_t relu;
+} sida_mx_gemm_config;
+int sida_mx_gemm(const sida_mx_gemm_config *cfg, const void *x_dev, const void *x_scales_dev, int64_t ldx, int32_t M,
+                 const void *codes_dev, const void *scales_dev, const int32_t *offsets_dev, void *y_dev, int64_t ldy, void *stream);
+
+/* ---- the router and its balance ---------------------------------------------------------------
+ * The ids and scaling factors of Eq. 1 (Section 2.1) where a router chooses them, and what trains one: the SoftMax
+ * p[t,:] of a token's E logits, its top_k experts (largest logits; ties to the lower expert id; a NaN counts as less than
+ * anything), their gates p[t, id] - divided by their sum where cfg->normalize is set -, the tokens per expert, and the
+ * balance loss of Switch layers
+ *     loss = E * sum_e f_e P_e,   f_e = counts[e] / (n * top_k),   P_e = sum_t p[t,e] / n,
+ * sums over the n tokens that take part; 0 where n = 0.  A token takes no part where mask_dev says 0 or where all its
+ * logits are -infinity: its gates are 0, nobody counts it, and its gradient is 0; its ids are still within [0,E).
+ * All arithmetic in fp32, sums in a fixed order: the same inputs give the same bits.
+ *   logits_dev  [T, E] of logits_type SIDA_BF16 or SIDA_FP32, rows ld values apart (ld >= E), at any address of such a value; on a
+ *               16-byte boundary, with 16-byte multiples between rows and E a multiple of 16 bytes, the calls are faster
+ *   mask_dev    NULL, or uint8 [T]
+ *   ids_dev     int32 [T, top_k], gates_dev fp32 [T, top_k]: what sida_moe_plan (after a copy to the host) and the
+ *               layer calls take (with sida_set_top_k); loss_dev fp32 [1]; counts_dev int32 [E], of the tokens that take part
+ *   workspace_dev  16-byte aligned, >= sida_route_workspace_bytes(cfg, T), scratch of this call alone until it is done
+ * Limits: E <= SIDA_MAX_E, top_k <= min(E, SIDA_MAX_TOP_K), 0 <= T <= 2^26, ld < 2^24. */
+typedef struct sida_route_config {
+    int32_t E, top_k;
+    int32_t logits_type;  /* SIDA_BF16 or SIDA_FP32 */
+    int32_t normalize;    /* gates of a token sum to one */
+} sida_route_config;
+size_t sida_route_workspace_bytes(const sida_route_config *cfg, int32_t T);      /* 0 on a bad config */
+int sida_route(const sida_route_config *cfg, const void *logits_dev, int64_t ld, int32_t T, const uint8_t *mask_dev,
+               int32_t *ids_dev, float *gates_dev, int32_t *counts_dev, float *loss_dev, void *workspace_dev,
+               size_t workspace_bytes, void *stream);
+/* Gradient of the logits: d_gates_dev fp32 [T, top_k] (NULL: none) and d_loss_dev fp32 [1] (NULL: none) are those of the gates and the
+ * loss; ids and counts are what sida_route has left for the same logits and mask (counts are constants of the loss).
+ *     d_logits[t,e] = p[t,e] * (g[t,e] - sum_j p[t,j] g[t,j]),
+ *     g[t,e] = d_loss * E/n * f_e + sum over the j with ids[t,j] = e of d_p[t,j],
+ *     d_p = d_gates, or with cfg->normalize (d_gates[t,j] - sum_i d_gates[t,i] gates[t,i]) / (sum of the chosen p)
+ * d_logits_dev [T, E] of logits_type, rows ld_d values apart (ld_d >= E); one rounding where it is bf16.  An id outside
+ * [0,E) adds nothing.  logits and d_logits may be the same array. */
+int sida_route_backward(const sida_route_config *cfg, const void *logits_dev, int64_t ld, int32_t T, const uint8_t *mask_dev,
+                        const int32_t *ids_dev, const int32_t *counts_dev, const float *d_gates_dev, const float *d_loss_dev,
+                        void *d_logits_dev, int64_t ld_d, void *stream);
+
 /* Inspection: the order in which a grouped-GEMM launch walks its output tiles.  For a launch over
  * m_tiles token tiles (the first m_tall of them belonging to experts with more than one tile) and
  * n_tiles_n weight-row tiles, fills token_tile[t], weight_tile[t] for t = 0 .. m_tiles*n_tiles_n-1

@@ -6,4 +6,6 @@ from .binding import (  # noqa: F401
     SIDA_MAX_E, K_NAMES, Context, SidaError, SidaPlan, SidaConfig, WsLayout, lib, lib_path,
     streams_create, streams_destroy, tile_order, SidaHashConfig, hash_param_count, hash_workspace_bytes,
     hash_forward, hash_forward_static,
+    BF16, FP32, MXFP4, MX_ROWS, MX_TILES, SidaMxGemmConfig, SidaRouteConfig, mx_codes_bytes, mx_scales_bytes, mx_quantize, mx_gemm,
+    route_workspace_bytes, route, route_backward,
 )

@@ -9,6 +9,8 @@ POLICY_FIFO, POLICY_LRU, POLICY_BELADY = 0, 1, 2
 POLICIES = {"fifo": POLICY_FIFO, "lru": POLICY_LRU, "belady": POLICY_BELADY}
 EAGAIN, ECLOSED = -6, -7
 DEBUG_CHECK_IDS, DEBUG_POISON_SLOTS = 1, 2
+BF16, FP32, MXFP4 = 0, 1, 2
+MX_ROWS, MX_TILES = 0, 1
 K_NAMES = ("sort", "gather", "gemm1", "gemm2", "combine", "copy")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -43,6 +45,14 @@ class SidaPlan(C.Structure):
 
 class SidaHashConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("d_model", "C", "L", "E", "top_k", "max_seq_len")]
+
+
+class SidaMxGemmConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("groups", "N", "K", "x_type", "y_type", "relu")]
+
+
+class SidaRouteConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("E", "top_k", "logits_type", "normalize")]
 
 
 class WsLayout(C.Structure):
@@ -105,6 +115,13 @@ def lib():
         "sida_combine": (C.c_int, [vp, vp, i32, vp, vp, sz, vp]),
         "sida_profile_enable": (C.c_int, [vp, i32]),
         "sida_profile_read": (C.c_int, [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64), i32]),
+        "sida_mx_codes_bytes": (sz, [C.c_int64, i32, i32]),
+        "sida_mx_scales_bytes": (sz, [C.c_int64, i32, i32]),
+        "sida_mx_quantize": (C.c_int, [vp, i32, C.c_int64, i32, C.c_int64, i32, vp, vp, vp, vp]),
+        "sida_mx_gemm": (C.c_int, [C.POINTER(SidaMxGemmConfig), vp, vp, C.c_int64, i32, vp, vp, vp, vp, C.c_int64, vp]),
+        "sida_route_workspace_bytes": (sz, [C.POINTER(SidaRouteConfig), i32]),
+        "sida_route": (C.c_int, [C.POINTER(SidaRouteConfig), vp, C.c_int64, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "sida_route_backward": (C.c_int, [C.POINTER(SidaRouteConfig), vp, C.c_int64, i32, vp, vp, vp, vp, vp, vp, C.c_int64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -163,6 +180,115 @@ def hash_forward_static(cfg: SidaHashConfig, params, x, n_seq, seq_len, ids, alp
                                         _stream(stream))
     if rc:
         raise SidaError(rc, "sida_hash_forward_static")
+
+
+# ---- experts in 4 bits and the router: torch tensors in, types and shapes from them.  What a C entry cannot see (a tensor's
+# type, its inner stride, its size) is checked here, the rest there.
+def _type(t) -> int:
+    kind = _TYPES.get(str(t.dtype))
+    if kind is None:
+        raise ValueError(f"bf16 or fp32 values are needed, not {t.dtype}")
+    return kind
+
+
+_TYPES = {"torch.bfloat16": BF16, "torch.float32": FP32}
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t, what: str):
+    """(rows, columns, values between rows) of a matrix whose rows are contiguous."""
+    _need(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.is_cuda, f"{what}: a matrix on the GPU with contiguous rows is needed")
+    rows, cols = t.shape
+    return rows, cols, t.stride(0) if rows > 1 else cols
+
+
+def _flat(t, n: int, kind: str, what: str):
+    """t holds at least n values of a type, one after the other."""
+    _need(str(t.dtype) in kind.split() and t.is_contiguous() and t.numel() >= n and t.is_cuda,
+          f"{what}: a contiguous tensor on the GPU of at least {n} values of type {kind} is needed")
+    return t.data_ptr()
+
+
+def mx_codes_bytes(rows: int, cols: int, layout: int) -> int:
+    return lib().sida_mx_codes_bytes(rows, cols, layout)
+
+
+def mx_scales_bytes(rows: int, cols: int, layout: int) -> int:
+    return lib().sida_mx_scales_bytes(rows, cols, layout)
+
+
+def mx_quantize(x, codes, scales, stream, layout=MX_ROWS, values=None):
+    """x: bf16 or fp32 [rows, cols]; codes, scales: uint8, mx_codes_bytes and mx_scales_bytes of them; values: bf16 [rows, cols] or None."""
+    L = lib()
+    rows, cols, ld = _rows(x, "x")
+    rc = L.sida_mx_quantize(x.data_ptr(), _type(x), rows, cols, ld, layout,
+                            _flat(codes, L.sida_mx_codes_bytes(rows, cols, layout), "torch.uint8", "codes"),
+                            _flat(scales, L.sida_mx_scales_bytes(rows, cols, layout), "torch.uint8", "scales"),
+                            0 if values is None else _flat(values, rows * cols, "torch.bfloat16", "values"), _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_mx_quantize")
+
+
+def mx_gemm(x, x_scales, codes, scales, offsets, y, stream, relu=False):
+    """x: bf16 [M, K], or uint8 [M, K/2] with x_scales; codes, scales: every group's matrix in tiles; offsets: int32 [groups + 1],
+    or None for one group; y: bf16 or fp32 [M, N]."""
+    L = lib()
+    x4 = x_scales is not None
+    _need(str(x.dtype) == ("torch.uint8" if x4 else "torch.bfloat16"), f"x: {'uint8 codes' if x4 else 'bf16 values'} are needed, not {x.dtype}")
+    M, K, ldx = _rows(x, "x")
+    if x4:
+        _need(ldx == K, "x: codes have to be contiguous")
+        K, ldx = 2 * K, 2 * ldx
+        x_scales = _flat(x_scales, L.sida_mx_scales_bytes(M, K, MX_ROWS), "torch.uint8", "x_scales")
+    rows, N, ldy = _rows(y, "y")
+    _need(rows == M, f"y: {M} rows are needed, not {rows}")
+    groups = 1 if offsets is None else offsets.numel() - 1
+    cfg = SidaMxGemmConfig(groups, N, K, MXFP4 if x4 else BF16, _type(y), 1 if relu else 0)
+    rc = L.sida_mx_gemm(C.byref(cfg), x.data_ptr(), x_scales or 0, ldx, M,
+                        _flat(codes, groups * L.sida_mx_codes_bytes(N, K, MX_TILES), "torch.uint8", "codes"),
+                        _flat(scales, groups * L.sida_mx_scales_bytes(N, K, MX_TILES), "torch.uint8", "scales"),
+                        0 if offsets is None else _flat(offsets, 1, "torch.int32", "offsets"), y.data_ptr(), ldy, _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_mx_gemm")
+
+
+def route_workspace_bytes(cfg: SidaRouteConfig, T: int) -> int:
+    return lib().sida_route_workspace_bytes(C.byref(cfg), T)
+
+
+def _route_args(logits, ids, counts, mask, normalize):
+    T, E, ld = _rows(logits, "logits")
+    _need(ids.dim() == 2 and ids.shape[0] == T, f"ids: [{T}, experts per token] are needed")
+    cfg = SidaRouteConfig(E, ids.shape[1], _type(logits), 1 if normalize else 0)
+    return (cfg, T, ld, 0 if mask is None else _flat(mask, T, "torch.bool torch.uint8", "mask"),
+            _flat(ids, ids.numel(), "torch.int32", "ids"), _flat(counts, E, "torch.int32", "counts"))
+
+
+def route(logits, ids, gates, counts, loss, workspace, stream, mask=None, normalize=False):
+    """logits: bf16 or fp32 [T, E]; ids: int32 [T, k]; gates: fp32 [T, k]; counts: int32 [E]; loss: fp32, one value; workspace:
+    route_workspace_bytes of it; mask: bool or uint8 [T] or None."""
+    cfg, T, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
+    rc = lib().sida_route(C.byref(cfg), logits.data_ptr(), ld, T, m, i, _flat(gates, ids.numel(), "torch.float32", "gates"), c,
+                          _flat(loss, 1, "torch.float32", "loss"), workspace.data_ptr(),
+                          workspace.numel() * workspace.element_size(), _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_route")
+
+
+def route_backward(logits, ids, counts, d_logits, stream, d_gates=None, d_loss=None, mask=None, normalize=False):
+    """d_logits: as logits; d_gates: fp32 [T, k] or None; d_loss: fp32, one value, or None."""
+    cfg, T, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
+    _need(d_logits.shape == logits.shape and d_logits.dtype == logits.dtype, "d_logits: shape and type of the logits are needed")
+    rc = lib().sida_route_backward(C.byref(cfg), logits.data_ptr(), ld, T, m, i, c,
+                                   0 if d_gates is None else _flat(d_gates, ids.numel(), "torch.float32", "d_gates"),
+                                   0 if d_loss is None else _flat(d_loss, 1, "torch.float32", "d_loss"),
+                                   d_logits.data_ptr(), _rows(d_logits, "d_logits")[2], _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_route_backward")
 
 
 def streams_create(copy_cus: int):

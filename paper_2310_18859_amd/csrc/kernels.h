@@ -133,4 +133,25 @@ int launch_hash_forward(const HashShape &sh, const float *params, const void *x,
 constexpr size_t kHashStaticScratchBytes = size_t(16) << 20;
 int hash_static_scratch(float **out);
 
+// Experts in 4 bits (mx_quant.hip, mx_gemm.hip); the arguments are those of the C calls, checked.
+int launch_mx_quantize(const void *x, bool fp32, int64_t rows, int32_t cols, int64_t ld, bool tiles, void *codes, void *scales,
+                       void *values, hipStream_t st);
+struct MxShape {
+    int32_t groups, N, K;
+    bool x4, y32, relu;
+};
+int launch_mx_gemm(const MxShape &sh, const void *x, const void *x_scales, int64_t ldx, int32_t M, const void *codes, const void *scales,
+                   const int32_t *offsets, void *y, int64_t ldy, hipStream_t st);
+
+// The router (route.hip).
+struct RouteShape {
+    int32_t E, top_k;
+    bool fp32, normalize;
+};
+int route_workgroups(int32_t T);   // workgroups of the forward pass: each leaves 8 bytes per expert in the workspace
+int launch_route(const RouteShape &s, const void *logits, int64_t ld, int32_t T, const uint8_t *mask, int32_t *ids, float *gates,
+                 int32_t *counts, float *loss, void *ws, hipStream_t st);
+int launch_route_backward(const RouteShape &s, const void *logits, int64_t ld, int32_t T, const uint8_t *mask, const int32_t *ids,
+                          const int32_t *counts, const float *d_gates, const float *d_loss, void *d_logits, int64_t ld_d, hipStream_t st);
+
 }  // namespace sida

@@ -1,0 +1,455 @@
+// The router: SoftMax of a token's expert logits, its top_k experts and their gates, tokens per expert and the balance loss
+//     loss = E * sum_e f_e P_e,   f_e = counts[e] / (n k),   P_e = sum_t p[t,e] / n
+// and the gradient of the logits.
+//
+// Sixteen lanes share a token, at most 16 logits each (E <= 256): a token's maximum and sums are four exchanges inside a row of
+// 16 lanes (full-rate register moves), four tokens to a wavefront.  With a wavefront to a token the six exchanges, two of
+// them through LDS, would cost more than the logits themselves.  All logits of a token are in registers at once, so every
+// pass reads them once.  exp(v - m) is 2^((v - m) log2 e), the difference first: m log2 e on its own would overflow where all logits
+// are the type's lowest value.
+//
+// Bound by bytes for large batches and by the launch for small ones; the vector operations per logit (about 10 forward, 14
+// backward, and 5 for each further expert per token) take half as long as the bytes do.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstddef>
+#include <cstdint>
+#include <type_traits>
+
+#include "kernels.h"
+
+namespace sida {
+
+namespace {
+
+constexpr int kLanes = 16;                     // lanes per token
+constexpr int kRouteThreads = 1024, kRouteRows = kRouteThreads / kLanes;
+constexpr int kRouteWaves = kRouteThreads / 64;
+constexpr int kMostE = 256;
+constexpr int kRouteBlocks = 256;              // workgroups whose sums the second launch adds: one per compute unit
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// Value of the lane N places on in the row of 16 lanes, around its end.
+template <int N>
+__device__ __forceinline__ float turned(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, true));
+}
+template <int N>
+__device__ __forceinline__ int turned(int v)
+{
+    return __builtin_amdgcn_mov_dpp(v, 0x120 + N, 0xf, 0xf, true);
+}
+// Each lane of the row gets the same bits: at every step the two sides add the same two numbers.
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += turned<8>(v);
+    v += turned<4>(v);
+    v += turned<2>(v);
+    return v + turned<1>(v);
+}
+__device__ __forceinline__ float row_max(float v)
+{
+    v = fmaxf(v, turned<8>(v));
+    v = fmaxf(v, turned<4>(v));
+    v = fmaxf(v, turned<2>(v));
+    return fmaxf(v, turned<1>(v));
+}
+__device__ __forceinline__ int row_min(int v)
+{
+    v = min(v, turned<8>(v));
+    v = min(v, turned<4>(v));
+    v = min(v, turned<2>(v));
+    return min(v, turned<1>(v));
+}
+__device__ __forceinline__ int row_sum(int v)
+{
+    v += turned<8>(v);
+    v += turned<4>(v);
+    v += turned<2>(v);
+    return v + turned<1>(v);
+}
+
+// A lane's logits: J loads of VEC values; load j of lane `sub` starts at column (j * 16 + sub) * VEC.  Places past E hold -infinity.
+template <class T, int VEC, int J>
+struct Row {
+    static constexpr int V = VEC * J;
+    typedef __attribute__((ext_vector_type(VEC))) T Vec;
+    float v[V];
+    static __device__ __forceinline__ int column(int sub, int i) { return ((i / VEC) * kLanes + sub) * VEC + i % VEC; }
+    __device__ __forceinline__ void load(const T *row, int sub, int E)
+    {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int c = (j * kLanes + sub) * VEC;
+            if (c < E) {                        // E is a multiple of VEC
+                if constexpr (VEC == 1) {
+                    v[j] = (float)row[c];
+                } else {
+                    const Vec x = *reinterpret_cast<const Vec *>(row + c);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) v[j * VEC + i] = (float)x[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[j * VEC + i] = -INFINITY;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T *row, int sub, int E) const
+    {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int c = (j * kLanes + sub) * VEC;
+            if (c < E) {
+                if constexpr (VEC == 1) {
+                    row[c] = (T)v[j];
+                } else {
+                    Vec x;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) x[i] = (T)v[j * VEC + i];
+                    *reinterpret_cast<Vec *>(row + c) = x;
+                }
+            }
+        }
+    }
+    // The largest logit that is a number, in every lane of the token; -infinity where there is none.
+    __device__ __forceinline__ float largest() const
+    {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < V; ++i) m = fmaxf(m, v[i]);
+        return row_max(m);
+    }
+    // Whether all logits are -infinity, given the largest.
+    __device__ __forceinline__ bool nothing(float m) const
+    {
+        if (m != -INFINITY) return false;
+        int nan = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) nan |= v[i] != v[i];
+        return row_sum(nan) == 0;
+    }
+};
+
+__device__ __forceinline__ float power(float v, float m) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); }
+
+struct RouteArgs {
+    const void *logits;
+    const uint8_t *mask;
+    int64_t ld, ld_d;
+    int T, E, k, normalize;
+    int32_t *ids;
+    float *gates;
+    int32_t *counts;
+    float *loss;
+    float *part_p;               // [workgroups][E]
+    int32_t *part_n;             // [workgroups][E]
+    const float *d_gates, *d_loss;
+    void *d_logits;
+};
+
+// counts and loss from the workgroups' sums, each expert's in the order of the workgroups within kSlices interleaved parts.
+constexpr int kSlices = kRouteThreads / kMostE;
+__device__ __forceinline__ void finish(const RouteArgs &a, int workgroups, float *p_sum, int *n_sum, float *terms, int *total)
+{
+    const int tid = threadIdx.x, e = tid % kMostE, slice = tid / kMostE;
+    float p = 0;
+    int n = 0;
+    if (e < a.E) {
+#pragma unroll 8
+        for (int b = slice; b < workgroups; b += kSlices) {
+            p += a.part_p[(size_t)b * a.E + e];
+            n += a.part_n[(size_t)b * a.E + e];
+        }
+    }
+    p_sum[tid] = p;
+    n_sum[tid] = n;
+    if (tid == 0) *total = 0;
+    __syncthreads();
+    if (tid < kMostE) {
+#pragma unroll
+        for (int s = 1; s < kSlices; ++s) {
+            p += p_sum[s * kMostE + tid];
+            n += n_sum[s * kMostE + tid];
+        }
+        if (tid < a.E) {
+            a.counts[tid] = n;
+            atomicAdd(total, n);
+        }
+        terms[tid] = p * (float)n;
+    }
+    __syncthreads();
+    for (int half = kMostE / 2; half > 0; half /= 2) {
+        if (tid < half) terms[tid] += terms[tid + half];
+        __syncthreads();
+    }
+    if (tid == 0) {
+        const float all = (float)*total, tokens = all / a.k;      // all = n k
+        *a.loss = *total ? (float)a.E * (terms[0] / all / tokens) : 0.f;
+    }
+}
+
+template <class T, int VEC, int J>
+__global__ __launch_bounds__(kRouteThreads) void route_rows(const RouteArgs a)
+{
+    typedef Row<T, VEC, J> R;
+    __shared__ float p_part[kRouteWaves][kMostE];
+    __shared__ int n_part[kMostE];
+    __shared__ float p_sum[kRouteThreads];
+    __shared__ int n_sum[kRouteThreads];
+    __shared__ float terms[kMostE];
+    __shared__ int total;
+    const int tid = threadIdx.x, sub = tid & (kLanes - 1), lane = tid & 63, wave = tid >> 6;
+    for (int e = tid; e < kMostE; e += kRouteThreads) n_part[e] = 0;
+    __syncthreads();
+    float p_acc[R::V];
+#pragma unroll
+    for (int i = 0; i < R::V; ++i) p_acc[i] = 0;
+    for (int64_t t = (int64_t)blockIdx.x * kRouteRows + tid / kLanes; t < a.T; t += (int64_t)gridDim.x * kRouteRows) {
+        R r;
+        r.load((const T *)a.logits + t * a.ld, sub, a.E);
+        const float m = r.largest();
+        const bool part = (!a.mask || a.mask[t]) && !r.nothing(m);
+        float e[R::V], sum = 0;
+#pragma unroll
+        for (int i = 0; i < R::V; ++i) {
+            e[i] = power(r.v[i], m);
+            sum += e[i];
+        }
+        const float inv = 1.f / row_sum(sum);
+        if (part) {
+#pragma unroll
+            for (int i = 0; i < R::V; ++i) p_acc[i] += e[i] * inv;
+        }
+        // The experts, one after the other: the largest logit left, the lowest column that has it.  A chosen logit becomes
+        // NaN, which no maximum takes.
+        int my_id = 0;
+        float my_gate = 0, gate_sum = 0, top = m;
+        uint32_t taken = 0;                                  // bit i: place i is chosen
+        for (int j = 0; j < a.k; ++j) {
+            if (j) top = r.largest();
+            int id = INT32_MAX;
+#pragma unroll
+            for (int i = R::V - 1; i >= 0; --i) id = r.v[i] == top ? R::column(sub, i) : id;
+            id = row_min(id);
+            if (id >= a.E) {                                 // only NaN are left: the lowest column not chosen yet
+                id = INT32_MAX;
+#pragma unroll
+                for (int i = R::V - 1; i >= 0; --i)
+                    if (!(taken >> i & 1) && R::column(sub, i) < a.E) id = R::column(sub, i);
+                id = row_min(id);
+            }
+            const float gate = power(top, m) * inv;
+            gate_sum += gate;
+            if (sub == j) {
+                my_id = id;
+                my_gate = gate;
+            }
+            if (j + 1 < a.k) {
+#pragma unroll
+                for (int i = 0; i < R::V; ++i) {
+                    const bool it = R::column(sub, i) == id;
+                    r.v[i] = it ? NAN : r.v[i];
+                    taken |= it ? 1u << i : 0u;
+                }
+            }
+        }
+        if (sub < a.k) {
+            if (a.normalize) my_gate /= gate_sum;
+            a.ids[t * a.k + sub] = my_id;
+            a.gates[t * a.k + sub] = part ? my_gate : 0.f;
+            if (part) atomicAdd(&n_part[my_id], 1);
+        }
+    }
+    // The four tokens of a wavefront, then the wavefronts, in a fixed order.
+#pragma unroll
+    for (int i = 0; i < R::V; ++i) {
+        p_acc[i] += __shfl_xor(p_acc[i], 16);
+        p_acc[i] += __shfl_xor(p_acc[i], 32);
+        if (lane < kLanes) p_part[wave][R::column(sub, i)] = p_acc[i];
+    }
+    __syncthreads();
+    if (tid < a.E) {
+        float p = 0;
+#pragma unroll
+        for (int w = 0; w < kRouteWaves; ++w) p += p_part[w][tid];
+        a.part_p[(size_t)blockIdx.x * a.E + tid] = p;
+        a.part_n[(size_t)blockIdx.x * a.E + tid] = n_part[tid];
+    }
+    if (gridDim.x == 1) {
+        __syncthreads();                                     // this workgroup's own stores
+        finish(a, 1, p_sum, n_sum, terms, &total);
+    }
+}
+
+__global__ __launch_bounds__(kRouteThreads) void route_finish(const RouteArgs a, int workgroups)
+{
+    __shared__ float p_sum[kRouteThreads];
+    __shared__ int n_sum[kRouteThreads];
+    __shared__ float terms[kMostE];
+    __shared__ int total;
+    finish(a, workgroups, p_sum, n_sum, terms, &total);
+}
+
+constexpr int kBackThreads = 256, kBackRows = kBackThreads / kLanes;
+template <class T, int VEC, int J>
+__global__ __launch_bounds__(kBackThreads) void route_back_rows(const RouteArgs a)
+{
+    typedef Row<T, VEC, J> R;
+    const int tid = threadIdx.x, sub = tid & (kLanes - 1);
+    // What the loss adds to an expert's column: d_loss E/n counts/(n k), n k being the sum of all counts.
+    float pull[R::V];
+    int all = 0;
+#pragma unroll
+    for (int i = 0; i < R::V; ++i) {
+        const int c = R::column(sub, i), n = c < a.E ? a.counts[c] : 0;
+        all += n;
+        pull[i] = (float)n;
+    }
+    all = row_sum(all);
+    const float nk = (float)all, coef = a.d_loss && all ? *a.d_loss * (float)a.E * (float)a.k / nk / nk : 0.f;
+#pragma unroll
+    for (int i = 0; i < R::V; ++i) pull[i] *= coef;
+    for (int64_t t = (int64_t)blockIdx.x * kBackRows + tid / kLanes; t < a.T; t += (int64_t)gridDim.x * kBackRows) {
+        const T *row = (const T *)a.logits + t * a.ld;
+        R r;
+        r.load(row, sub, a.E);
+        const float m = r.largest();
+        const bool part = (!a.mask || a.mask[t]) && !r.nothing(m);
+        float p[R::V], sum = 0;
+#pragma unroll
+        for (int i = 0; i < R::V; ++i) {
+            p[i] = power(r.v[i], m);
+            sum += p[i];
+        }
+        const float inv = 1.f / row_sum(sum);
+        float d[R::V];
+#pragma unroll
+        for (int i = 0; i < R::V; ++i) {
+            p[i] *= inv;
+            d[i] = pull[i];
+        }
+        if (a.d_gates) {
+            const int32_t *ids = a.ids + t * a.k;
+            const float *dg = a.d_gates + t * a.k;
+            float mean = 0, scale = 1;
+            if (a.normalize) {                               // sum_i dg_i gate_i, and one over the sum of the chosen p
+                float chosen = 0;
+                for (int j = 0; j < a.k; ++j) {
+                    const int id = ids[j];
+                    if ((uint32_t)id >= (uint32_t)a.E) continue;
+                    const float q = power((float)row[id], m) * inv;
+                    chosen += q;
+                    mean += dg[j] * q;
+                }
+                scale = 1.f / chosen;
+                mean *= scale;
+            }
+            for (int j = 0; j < a.k; ++j) {
+                const int id = (uint32_t)ids[j] < (uint32_t)a.E ? ids[j] : -1;   // a place past E is no expert's
+                const float g = (dg[j] - mean) * scale;
+#pragma unroll
+                for (int i = 0; i < R::V; ++i) d[i] += R::column(sub, i) == id ? g : 0.f;
+            }
+        }
+        float dot = 0;
+#pragma unroll
+        for (int i = 0; i < R::V; ++i) dot += p[i] * d[i];
+        dot = row_sum(dot);
+#pragma unroll
+        for (int i = 0; i < R::V; ++i) r.v[i] = part ? p[i] * (d[i] - dot) : 0.f;
+        r.store((T *)a.d_logits + t * a.ld_d, sub, a.E);
+    }
+}
+
+template <class T, int VEC, int J>
+int launch_forward(const RouteArgs &a, hipStream_t st)
+{
+    const int grid = route_workgroups(a.T);
+    route_rows<T, VEC, J><<<grid, kRouteThreads, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && grid > 1) {
+        route_finish<<<1, kRouteThreads, 0, st>>>(a, grid);
+        e = hipGetLastError();
+    }
+    return (int)e;
+}
+template <class T, int VEC, int J>
+int launch_back(const RouteArgs &a, hipStream_t st)
+{
+    const int64_t need = ((int64_t)a.T + kBackRows - 1) / kBackRows;
+    route_back_rows<T, VEC, J><<<(int)(need < 8192 ? need : 8192), kBackThreads, 0, st>>>(a);
+    return (int)hipGetLastError();
+}
+
+// Picks the loads per lane.  16-byte loads where every row starts on a 16-byte boundary and E is a multiple of a load's values.
+template <class T, class Use>
+int by_width(const RouteArgs &a, bool wide, Use &&use)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    if (wide) {
+        const int j = (a.E + kLanes * VEC - 1) / (kLanes * VEC);
+        if (j <= 1) return use(std::integral_constant<int, VEC>(), std::integral_constant<int, 1>());
+        if (j <= 2) return use(std::integral_constant<int, VEC>(), std::integral_constant<int, 2>());
+        if constexpr (VEC == 4) return use(std::integral_constant<int, VEC>(), std::integral_constant<int, 4>());
+    }
+    const int j = (a.E + kLanes - 1) / kLanes;
+    if (j <= 2) return use(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+    if (j <= 4) return use(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+    if (j <= 8) return use(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+    return use(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
+}
+template <class T>
+bool rows_wide(const void *p, int64_t ld, int E)
+{
+    return (((uintptr_t)p | (uintptr_t)ld * sizeof(T)) % 16) == 0 && E % (16 / sizeof(T)) == 0;
+}
+template <class T>
+int forward_typed(const RouteArgs &a, hipStream_t st)
+{
+    return by_width<T>(a, rows_wide<T>(a.logits, a.ld, a.E),
+                       [&](auto vec, auto j) { return launch_forward<T, decltype(vec)::value, decltype(j)::value>(a, st); });
+}
+template <class T>
+int back_typed(const RouteArgs &a, hipStream_t st)
+{
+    return by_width<T>(a, rows_wide<T>(a.logits, a.ld, a.E) && rows_wide<T>(a.d_logits, a.ld_d, a.E),
+                       [&](auto vec, auto j) { return launch_back<T, decltype(vec)::value, decltype(j)::value>(a, st); });
+}
+
+}  // namespace
+
+// Up to kRouteOne tokens one workgroup does everything: the second launch costs more than its rounds of 64 tokens.
+constexpr int kRouteOne = 256;
+int route_workgroups(int32_t T)
+{
+    if (T <= kRouteOne) return 1;
+    const int need = (int)(((int64_t)T + kRouteRows - 1) / kRouteRows);
+    return need < kRouteBlocks ? need : kRouteBlocks;
+}
+
+int launch_route(const RouteShape &s, const void *logits, int64_t ld, int32_t T, const uint8_t *mask, int32_t *ids, float *gates,
+                 int32_t *counts, float *loss, void *ws, hipStream_t st)
+{
+    RouteArgs a{};
+    a.logits = logits, a.ld = ld, a.T = T, a.E = s.E, a.k = s.top_k, a.normalize = s.normalize, a.mask = mask;
+    a.ids = ids, a.gates = gates, a.counts = counts, a.loss = loss;
+    a.part_p = (float *)ws;
+    a.part_n = (int32_t *)(a.part_p + (size_t)route_workgroups(T) * s.E);
+    return s.fp32 ? forward_typed<float>(a, st) : forward_typed<__bf16>(a, st);
+}
+
+int launch_route_backward(const RouteShape &s, const void *logits, int64_t ld, int32_t T, const uint8_t *mask, const int32_t *ids,
+                          const int32_t *counts, const float *d_gates, const float *d_loss, void *d_logits, int64_t ld_d,
+                          hipStream_t st)
+{
+    RouteArgs a{};
+    a.logits = logits, a.ld = ld, a.T = T, a.E = s.E, a.k = s.top_k, a.normalize = s.normalize, a.mask = mask;
+    a.ids = const_cast<int32_t *>(ids), a.counts = const_cast<int32_t *>(counts);
+    a.d_gates = d_gates, a.d_loss = d_loss, a.d_logits = d_logits, a.ld_d = ld_d;
+    return s.fp32 ? back_typed<float>(a, st) : back_typed<__bf16>(a, st);
+}
+
+}  // namespace sida
