@@ -3,6 +3,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -26,18 +27,31 @@ struct MxArgs {
     int64_t ldx, ldy;            // values between rows
     int64_t code_bytes, scale_bytes;   // between experts
     int M, N, K, groups;
+    int relu, whole_lines;       // whole_lines: rows of y start on 16-byte boundaries, N is a multiple of 32
 };
 
-// Which rows tile `mt` of BM rows is: tiles are counted group by group.  Every wavefront finds it for itself, four groups to
-// a lane; rows = 0 where there are fewer tiles.
-struct TokenTile {
-    int group, row0, rows;
+// Which tile a workgroup takes.  Token tiles are counted group by group (BM rows each, a group's last one less), and each has
+// n_tiles column tiles.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles there are, one after the other, so
+// that a token tile's rows and a group's matrix are fetched into one L2.  Every wavefront finds its tile by itself, four groups to
+// a lane; rows = 0 where there are fewer tiles than workgroups.
+struct Placed {
+    int group, row0, rows, nt;
 };
 template <int BM>
-__device__ __forceinline__ TokenTile find_tile(const MxArgs &a, int mt)
+__device__ __forceinline__ Placed place(const MxArgs &a, int n_tiles)
 {
-    if (!a.offsets) return TokenTile{0, mt * BM, max(0, min(BM, a.M - mt * BM))};
     const int lane = threadIdx.x & 63;
+    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    auto tile_of = [&](int tiles) {                          // (token tile, column tile), or -1
+        const int total = tiles * n_tiles, share = (total + 7) / 8, id = xcd * share + local;
+        return local < share && id < total ? id : -1;
+    };
+    if (!a.offsets) {
+        const int id = tile_of((a.M + BM - 1) / BM);
+        if (id < 0) return Placed{0, 0, 0, 0};
+        const int row0 = id / n_tiles * BM;
+        return Placed{0, row0, min(BM, a.M - row0), id % n_tiles};
+    }
     int at[5];
 #pragma unroll
     for (int i = 0; i < 5; ++i) at[i] = max(0, min(a.M, a.offsets[min(lane * 4 + i, a.groups)]));
@@ -50,9 +64,10 @@ __device__ __forceinline__ TokenTile find_tile(const MxArgs &a, int mt)
         const int v = __shfl_up(before, d);
         if (lane >= d) before += v;
     }
-    const uint64_t later = __ballot(before > mt);
-    if (later == 0) return TokenTile{0, 0, 0};
-    const int owner = __builtin_ctzll(later);
+    const int id = tile_of(__builtin_amdgcn_readlane(before, 63));
+    if (id < 0) return Placed{0, 0, 0, 0};
+    const int mt = id / n_tiles;
+    const int owner = __builtin_ctzll(__ballot(before > mt));
     int left = mt - (before - tiles), group = 0, row0 = 0, rows = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -64,8 +79,7 @@ __device__ __forceinline__ TokenTile find_tile(const MxArgs &a, int mt)
         }
         left -= n;
     }
-    return TokenTile{__builtin_amdgcn_readfirstlane(__shfl(group, owner)), __builtin_amdgcn_readfirstlane(__shfl(row0, owner)),
-                     __builtin_amdgcn_readfirstlane(__shfl(rows, owner))};
+    return Placed{__builtin_amdgcn_readlane(group, owner), __builtin_amdgcn_readlane(row0, owner), __builtin_amdgcn_readlane(rows, owner), id % n_tiles};
 }
 
 // Eight codes times their power of two, exact in bf16.
@@ -79,65 +93,245 @@ __device__ __forceinline__ bf16x8 decode(uint32_t c, float s)
     return o;
 }
 
+__device__ __forceinline__ i32x8 wide(i32x4 v) { return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }   // 4-bit operands fill half of the registers
 __device__ __forceinline__ float relu_of(float v) { return v <= 0.f ? 0.f : v; }   // NaN stays
 
-// One wavefront: 32 tokens x 32 columns, operands straight from memory.
-template <bool X4, class Y, bool RELU>
-__global__ __launch_bounds__(256) void mx_gemm_simple(const MxArgs a)
+template <int N>
+__device__ __forceinline__ void wait_loads()
 {
-    const int lane = threadIdx.x & 63, half = lane >> 5, stripe = blockIdx.y * 4 + (threadIdx.x >> 6);
-    const TokenTile t = find_tile<32>(a, blockIdx.x);
-    if (t.rows == 0 || stripe * 32 >= a.N) return;
-    const int steps = (a.K + 63) / 64;
-    const char *w = a.codes + t.group * a.code_bytes + (size_t)stripe * steps * 1024 + lane * 16;
-    const char *ws = a.scales + t.group * a.scale_bytes + (size_t)stripe * ((a.K + 255) / 256) * 256 + lane * 4;
-    const int row = t.row0 + min(lane & 31, t.rows - 1);
-    const int pitch = (a.K + 255) / 256 * 8;
-    f32x16 acc;
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
+}
+// 16 or 4 bytes per lane straight into LDS: lane i's land at dst + 16 * i or 4 * i.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t offset, void *dst)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 16, (int)offset, 0, 0, 0);
+}
+__device__ __forceinline__ void load_word_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t offset, void *dst)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 4, (int)offset, 0, 0, 0);
+}
+// Lane offset of a load that asks for nothing: past every descriptor here (128 rows less than 2^25 bytes apart).
+constexpr uint32_t kNowhere = 0xffffff00u;
+
+constexpr int kWaves = 4;
+constexpr int kStageRow = 128;                 // bytes of a token row per stage: 64 values in bf16, 256 in 4 bits
+
+// A workgroup of four wavefronts: 32 MI tokens x 128 NS columns; wavefront w owns NS stripes of 32 columns and all tokens.
+template <bool X4, int MI, int NS, int NB, int WB, class Y>
+__global__ __launch_bounds__(kWaves * 64, 2) void mx_gemm_tiles(const MxArgs a)
+{
+    constexpr int BM = 32 * MI, BN = 32 * NS * kWaves;
+    constexpr int kStage = BM * kStageRow + (X4 ? 1024 : 0);   // token rows, and their scales
+    constexpr int kRing = (NB + 1) * kStage;
+    constexpr int kTurnCols = sizeof(Y) == 2 ? NS * 32 : 32;   // columns that go through LDS together
+    constexpr int kTurnPitch = kTurnCols * (int)sizeof(Y) + 16;
+    constexpr int kTurn = kWaves * 32 * kTurnPitch;
+    constexpr int WQ = X4 ? 4 : 1;                             // weight fragments per stripe and stage
+    // After a stage's token loads at least the token loads of NB - 1 later stages and WB stages of weights are asked for
+    // before it is used; the waits for the weights themselves are the compiler's.
+    constexpr int kLater = (NB - 1) * (MI + (X4 ? 1 : 0)) + WB * NS * (WQ + 1);
+    static_assert(kLater <= 63 && NB % WB == 0, "vmcnt range");
+    __shared__ __attribute__((aligned(1024))) char lds[kRing > kTurn ? kRing : kTurn];
+
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n_tiles = (a.N + BN - 1) / BN;
+    const Placed at = place<BM>(a, n_tiles);
+    if (at.rows == 0) return;
+    const int stripe0 = at.nt * (NS * kWaves) + wv * NS, stripes = (a.N + 31) / 32;
+    const int chunks = (a.K + 63) / 64, groups = (a.K + 255) / 256;
+    const int row_bytes = X4 ? a.K / 2 : a.K * 2;
+    const int stages = (row_bytes + kStageRow - 1) / kStageRow;
+
+    // token loads: a wavefront's load j brings rows 8 (wv MI + j) .. + 7; row r's piece c goes to place c ^ (r / 2 & 7)
+    const uint32_t pitch = X4 ? (uint32_t)row_bytes : (uint32_t)a.ldx * 2;
+    const char *x = a.x + (int64_t)at.row0 * pitch;
+    uint32_t tok_off[MI];
+    int tok_piece[MI];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0;
-    for (int s = 0; s < steps; ++s) {
-        const i32x4 c = *reinterpret_cast<const i32x4 *>(w + (size_t)s * 1024);
-        const uint32_t scale = (uint8_t)ws[(s / 4) * 256 + s % 4];
-        const int k = s * 64 + half * 32;
-        const bool in = k < a.K;
+    for (int j = 0; j < MI; ++j) {
+        const int r = (wv * MI + j) * 8 + (lane >> 3);
+        tok_piece[j] = ((lane & 7) ^ (r >> 1 & 7)) * 16;
+        tok_off[j] = r < at.rows ? (uint32_t)r * pitch + tok_piece[j] : kNowhere;
+    }
+    const uint32_t span = (uint32_t)(at.rows - 1) * pitch + row_bytes;
+    const int scale_pitch = groups * 8;
+    const __amdgpu_buffer_rsrc_t xs_rsrc = make_rsrc(a.x_scales + (X4 ? (int64_t)at.row0 * scale_pitch : 0), (uint32_t)at.rows * scale_pitch);
+    const uint32_t xs_off = wv * 32 + (lane >> 1) < BM ? (uint32_t)(wv * 32 + (lane >> 1)) * scale_pitch + (lane & 1) * 4 : kNowhere;
+    auto load_tokens = [&](int stage) {
+        char *dst = lds + stage % (NB + 1) * kStage;
+        const __amdgpu_buffer_rsrc_t r = make_rsrc(x + (int64_t)stage * kStageRow, span);
+#pragma unroll
+        for (int j = 0; j < MI; ++j)
+            load_to_lds(r, stage * kStageRow + tok_piece[j] < row_bytes ? tok_off[j] : kNowhere, dst + (wv * MI + j) * 1024);
+        if (X4) load_word_to_lds(xs_rsrc, stage < stages && xs_off != kNowhere ? xs_off + stage * 8 : kNowhere, dst + BM * kStageRow + wv * 256);
+    };
+
+    __amdgpu_buffer_rsrc_t w_rsrc[NS], s_rsrc[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const bool in = stripe0 + s < stripes;
+        const int64_t st = in ? stripe0 + s : 0;
+        w_rsrc[s] = make_rsrc(a.codes + at.group * a.code_bytes + st * chunks * 1024, in ? chunks * 1024 : 0);
+        s_rsrc[s] = make_rsrc(a.scales + at.group * a.scale_bytes + st * groups * 256, in ? groups * 256 : 0);
+    }
+    i32x4 w[WB][NS][WQ];
+    uint32_t ws[WB][NS];
+    auto load_weights = [&](int b, int stage) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+#pragma unroll
+            for (int q = 0; q < WQ; ++q)
+                w[b][s][q] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc[s], lane * 16 + stage * (WQ * 1024) + q * 1024, 0, 0));
+            if (X4) ws[b][s] = __builtin_amdgcn_raw_buffer_load_b32(s_rsrc[s], lane * 4 + stage * 256, 0, 0);
+            else ws[b][s] = __builtin_amdgcn_raw_buffer_load_b8(s_rsrc[s], lane * 4 + (stage >> 2) * 256 + (stage & 3), 0, 0);
+        }
+    };
+
+    f32x16 acc[NS][MI];
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int m = 0; m < MI; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[s][m][r] = 0;
+    const int live = (at.rows + 31) / 32;
+    int frag_off[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) frag_off[q] = (lane & 31) * kStageRow + (((X4 ? 2 * q + half : half * 4 + q) ^ ((lane & 31) >> 1 & 7)) * 16);
+    auto multiply = [&](int b, int stage) {
+        const char *src = lds + stage % (NB + 1) * kStage;
         if constexpr (X4) {
-            i32x4 x = {0, 0, 0, 0};
-            uint32_t xs = 127;
-            if (in) {
-                x = *reinterpret_cast<const i32x4 *>(a.x + (size_t)row * (a.K / 2) + k / 2);
-                xs = a.x_scales[(size_t)row * pitch + k / 32];
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+            uint32_t xs[MI];
+#pragma unroll
+            for (int m = 0; m < MI; ++m) {
+                const u32x2 both = *reinterpret_cast<const u32x2 *>(src + BM * kStageRow + (m * 32 + (lane & 31)) * 8);
+                xs[m] = __builtin_amdgcn_perm(both[1], both[0], half ? 0x07050301u : 0x06040200u);
             }
-            const i32x8 c8 = {c[0], c[1], c[2], c[3], 0, 0, 0, 0}, x8 = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
-            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(c8, x8, acc, 4, 4, 0, scale, 0, xs);
+            auto step = [&](auto place) {
+                constexpr int q = decltype(place)::value;
+#pragma unroll
+                for (int m = 0; m < MI; ++m) {
+                    if (m >= live) break;
+                    const i32x4 x = *reinterpret_cast<const i32x4 *>(src + m * 32 * kStageRow + frag_off[q]);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s)
+                        acc[s][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(w[b][s][q]), wide(x), acc[s][m], 4, 4, q, ws[b][s], q, xs[m]);
+                }
+            };
+            step(std::integral_constant<int, 0>());
+            step(std::integral_constant<int, 1>());
+            step(std::integral_constant<int, 2>());
+            step(std::integral_constant<int, 3>());
         } else {
-            const float f = __builtin_bit_cast(float, scale << 23);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                bf16x8 x;
+                bf16x8 v[NS];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = (__bf16)0.f;
-                if (in) x = *reinterpret_cast<const bf16x8 *>(a.x + ((size_t)row * a.ldx + k + q * 8) * 2);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(c[q], f), x, acc, 0, 0, 0);
+                for (int s = 0; s < NS; ++s) v[s] = decode(w[b][s][0][q], __builtin_bit_cast(float, ws[b][s] << 23));
+#pragma unroll
+                for (int m = 0; m < MI; ++m) {
+                    if (m >= live) break;
+                    const bf16x8 x = *reinterpret_cast<const bf16x8 *>(src + m * 32 * kStageRow + frag_off[q]);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) acc[s][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[s], x, acc[s][m], 0, 0, 0);
+                }
             }
         }
-    }
-    if ((lane & 31) >= t.rows) return;
-    Y *y = (Y *)a.y + (size_t)row * a.ldy;
+    };
+
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int col = stripe * 32 + 8 * (r / 4) + 4 * half + r % 4;
-        if (col < a.N) y[col] = (Y)(RELU ? relu_of(acc[r]) : acc[r]);
+    for (int i = 0; i < NB; ++i) load_tokens(i);
+#pragma unroll
+    for (int i = 0; i < WB; ++i) load_weights(i, i);
+    for (int t = 0; t < stages; t += NB) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            wait_loads<kLater>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            load_tokens(t + i + NB);
+            multiply(i % WB, t + i);
+            load_weights(i % WB, t + i + WB);
+        }
+    }
+    wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+
+    // Results.  A lane holds four times four consecutive columns of one token.
+    Y *y = (Y *)a.y + (int64_t)at.row0 * a.ldy;
+    if (a.whole_lines) {
+        char *turn = lds + wv * 32 * kTurnPitch;
+        constexpr int kPer = kTurnCols / 32;                    // stripes per turn
+        constexpr int kLanes = kTurnCols * (int)sizeof(Y) / 16; // lanes per row piece
+#pragma unroll
+        for (int m = 0; m < MI; ++m) {
+            if (m >= live) break;
+#pragma unroll
+            for (int s0 = 0; s0 < NS; s0 += kPer) {
+#pragma unroll
+                for (int s = 0; s < kPer; ++s)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        typedef __attribute__((ext_vector_type(4))) Y Y4;
+                        Y4 v;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float e = acc[s0 + s][m][4 * q + j];
+                            v[j] = (Y)(a.relu ? relu_of(e) : e);
+                        }
+                        *reinterpret_cast<Y4 *>(turn + (lane & 31) * kTurnPitch + (s * 32 + q * 8 + half * 4) * (int)sizeof(Y)) = v;
+                    }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int i = 0; i < 32 * kLanes / 64; ++i) {
+                    const int r = i * (64 / kLanes) + lane / kLanes, c = lane % kLanes * (16 / (int)sizeof(Y));
+                    const i32x4 v = *reinterpret_cast<const i32x4 *>(turn + r * kTurnPitch + c * (int)sizeof(Y));
+                    const int col = (stripe0 + s0) * 32 + c;
+                    if (m * 32 + r < at.rows && col < a.N) *reinterpret_cast<i32x4 *>(y + (int64_t)(m * 32 + r) * a.ldy + col) = v;
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    } else {
+#pragma unroll
+        for (int m = 0; m < MI; ++m) {
+            const int r = m * 32 + (lane & 31);
+            if (r >= at.rows) continue;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int col = (stripe0 + s) * 32 + 8 * (j / 4) + 4 * half + j % 4;
+                    const float e = acc[s][m][j];
+                    if (col < a.N) y[(int64_t)r * a.ldy + col] = (Y)(a.relu ? relu_of(e) : e);
+                }
+        }
     }
 }
 
-template <bool X4, class Y>
-int launch_typed(const MxArgs &a, bool relu, hipStream_t st)
+template <bool X4, int MI, int NS, int NB, int WB, class Y>
+int launch_shape(const MxArgs &a, hipStream_t st)
 {
-    const dim3 grid(a.M / 32 + (a.groups < a.M ? a.groups : a.M), (a.N + 127) / 128);
-    if (relu) mx_gemm_simple<X4, Y, true><<<grid, 256, 0, st>>>(a);
-    else mx_gemm_simple<X4, Y, false><<<grid, 256, 0, st>>>(a);
+    constexpr int BM = 32 * MI, BN = 32 * NS * kWaves;
+    const int64_t tiles = a.M / BM + (a.groups < a.M ? a.groups : a.M), grid = tiles * ((a.N + BN - 1) / BN);
+    mx_gemm_tiles<X4, MI, NS, NB, WB, Y><<<(uint32_t)((grid + 7) / 8 * 8), kWaves * 64, 0, st>>>(a);
     return (int)hipGetLastError();
+}
+
+template <bool X4, class Y>
+int launch_typed(const MxArgs &a, hipStream_t st)
+{
+    const int mean = a.M / a.groups;
+    const int mi = mean > 64 ? (X4 ? 4 : 2) : mean > 32 ? 2 : 1;
+    if (X4 && mi == 4) return launch_shape<X4, 4, 2, 2, 1, Y>(a, st);
+    if (mi == 2) return launch_shape<X4, 2, 2, 2, 2, Y>(a, st);
+    return launch_shape<X4, 1, 1, X4 ? 2 : 4, X4 ? 2 : 4, Y>(a, st);
 }
 
 }  // namespace
@@ -151,8 +345,11 @@ int launch_mx_gemm(const MxShape &sh, const void *x, const void *x_scales, int64
     const int64_t n = (sh.N + 31) / 32 * 32;
     a.code_bytes = n * ((sh.K + 63) / 64 * 32);
     a.scale_bytes = n * ((sh.K + 255) / 256 * 8);
-    if (sh.x4) return sh.y32 ? launch_typed<true, float>(a, sh.relu, st) : launch_typed<true, __bf16>(a, sh.relu, st);
-    return sh.y32 ? launch_typed<false, float>(a, sh.relu, st) : launch_typed<false, __bf16>(a, sh.relu, st);
+    a.relu = sh.relu;
+    const size_t size = sh.y32 ? 4 : 2;
+    a.whole_lines = ((uintptr_t)y | (size_t)ldy * size) % 16 == 0 && sh.N % 32 == 0;
+    if (sh.x4) return sh.y32 ? launch_typed<true, float>(a, st) : launch_typed<true, __bf16>(a, st);
+    return sh.y32 ? launch_typed<false, float>(a, st) : launch_typed<false, __bf16>(a, st);
 }
 
 }  // namespace sida
