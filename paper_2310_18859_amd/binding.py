@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 SIDA_MAX_E = 256
@@ -184,32 +185,39 @@ def hash_forward_static(cfg: SidaHashConfig, params, x, n_seq, seq_len, ids, alp
 
 # ---- experts in 4 bits and the router: torch tensors in, types and shapes from them.  What a C entry cannot see (a tensor's
 # type, its inner stride, its size) is checked here, the rest there.
+_KINDS = {}                              # torch.dtype -> SIDA_BF16 / SIDA_FP32, and the dtypes by name; filled at the first call
+
+
+def _kinds():
+    if not _KINDS:
+        import torch
+        _KINDS.update({torch.bfloat16: BF16, torch.float32: FP32, "bf16": (torch.bfloat16,), "fp32": (torch.float32,), "uint8": (torch.uint8,),
+                       "int32": (torch.int32,), "bool": (torch.bool, torch.uint8)})
+    return _KINDS
+
+
 def _type(t) -> int:
-    kind = _TYPES.get(str(t.dtype))
+    kind = _kinds().get(t.dtype)
     if kind is None:
         raise ValueError(f"bf16 or fp32 values are needed, not {t.dtype}")
     return kind
 
 
-_TYPES = {"torch.bfloat16": BF16, "torch.float32": FP32}
-
-
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
-
-
 def _rows(t, what: str):
-    """(rows, columns, values between rows) of a matrix whose rows are contiguous."""
-    _need(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.is_cuda, f"{what}: a matrix on the GPU with contiguous rows is needed")
+    """(rows, columns, values between rows) of a matrix on the GPU whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: a matrix on the GPU is needed")
     rows, cols = t.shape
-    return rows, cols, t.stride(0) if rows > 1 else cols
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{what}: contiguous rows are needed")
+    return rows, cols, ld if rows > 1 else cols
 
 
 def _flat(t, n: int, kind: str, what: str):
-    """t holds at least n values of a type, one after the other."""
-    _need(str(t.dtype) in kind.split() and t.is_contiguous() and t.numel() >= n and t.is_cuda,
-          f"{what}: a contiguous tensor on the GPU of at least {n} values of type {kind} is needed")
+    """Address of t, which holds at least n values of a type, one after the other, on the GPU."""
+    if t.dtype not in _kinds()[kind] or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: a contiguous tensor of at least {n} {kind} values on the GPU is needed")
     return t.data_ptr()
 
 
@@ -221,14 +229,30 @@ def mx_scales_bytes(rows: int, cols: int, layout: int) -> int:
     return lib().sida_mx_scales_bytes(rows, cols, layout)
 
 
+@functools.lru_cache(maxsize=1024)
+def _mx_bytes(rows: int, cols: int, layout: int):
+    return lib().sida_mx_codes_bytes(rows, cols, layout), lib().sida_mx_scales_bytes(rows, cols, layout)
+
+
+@functools.lru_cache(maxsize=1024)
+def _gemm_config(*fields):
+    cfg = SidaMxGemmConfig(*fields)
+    return cfg, C.byref(cfg)
+
+
+@functools.lru_cache(maxsize=1024)
+def _route_config(*fields):
+    cfg = SidaRouteConfig(*fields)
+    return cfg, C.byref(cfg)
+
+
 def mx_quantize(x, codes, scales, stream, layout=MX_ROWS, values=None):
     """x: bf16 or fp32 [rows, cols]; codes, scales: uint8, mx_codes_bytes and mx_scales_bytes of them; values: bf16 [rows, cols] or None."""
-    L = lib()
     rows, cols, ld = _rows(x, "x")
-    rc = L.sida_mx_quantize(x.data_ptr(), _type(x), rows, cols, ld, layout,
-                            _flat(codes, L.sida_mx_codes_bytes(rows, cols, layout), "torch.uint8", "codes"),
-                            _flat(scales, L.sida_mx_scales_bytes(rows, cols, layout), "torch.uint8", "scales"),
-                            0 if values is None else _flat(values, rows * cols, "torch.bfloat16", "values"), _stream(stream))
+    n_codes, n_scales = _mx_bytes(rows, cols, layout)
+    rc = lib().sida_mx_quantize(x.data_ptr(), _type(x), rows, cols, ld, layout, _flat(codes, n_codes, "uint8", "codes"),
+                                _flat(scales, n_scales, "uint8", "scales"),
+                                None if values is None else _flat(values, rows * cols, "bf16", "values"), _stream(stream))
     if rc:
         raise SidaError(rc, "sida_mx_quantize")
 
@@ -236,22 +260,23 @@ def mx_quantize(x, codes, scales, stream, layout=MX_ROWS, values=None):
 def mx_gemm(x, x_scales, codes, scales, offsets, y, stream, relu=False):
     """x: bf16 [M, K], or uint8 [M, K/2] with x_scales; codes, scales: every group's matrix in tiles; offsets: int32 [groups + 1],
     or None for one group; y: bf16 or fp32 [M, N]."""
-    L = lib()
-    x4 = x_scales is not None
-    _need(str(x.dtype) == ("torch.uint8" if x4 else "torch.bfloat16"), f"x: {'uint8 codes' if x4 else 'bf16 values'} are needed, not {x.dtype}")
     M, K, ldx = _rows(x, "x")
-    if x4:
-        _need(ldx == K, "x: codes have to be contiguous")
-        K, ldx = 2 * K, 2 * ldx
-        x_scales = _flat(x_scales, L.sida_mx_scales_bytes(M, K, MX_ROWS), "torch.uint8", "x_scales")
     rows, N, ldy = _rows(y, "y")
-    _need(rows == M, f"y: {M} rows are needed, not {rows}")
+    kind, xs = BF16, None
+    if x_scales is not None:
+        if ldx != K:
+            raise ValueError("x: codes have to be contiguous")
+        K, ldx, kind = 2 * K, 2 * ldx, MXFP4
+        xs = _flat(x_scales, _mx_bytes(M, K, MX_ROWS)[1], "uint8", "x_scales")
+    if x.dtype not in _kinds()["bf16" if xs is None else "uint8"]:
+        raise ValueError(f"x: bf16 values, or uint8 codes with their scales, are needed, not {x.dtype}")
+    if rows != M:
+        raise ValueError(f"y: {M} rows are needed, not {rows}")
     groups = 1 if offsets is None else offsets.numel() - 1
-    cfg = SidaMxGemmConfig(groups, N, K, MXFP4 if x4 else BF16, _type(y), 1 if relu else 0)
-    rc = L.sida_mx_gemm(C.byref(cfg), x.data_ptr(), x_scales or 0, ldx, M,
-                        _flat(codes, groups * L.sida_mx_codes_bytes(N, K, MX_TILES), "torch.uint8", "codes"),
-                        _flat(scales, groups * L.sida_mx_scales_bytes(N, K, MX_TILES), "torch.uint8", "scales"),
-                        0 if offsets is None else _flat(offsets, 1, "torch.int32", "offsets"), y.data_ptr(), ldy, _stream(stream))
+    n_codes, n_scales = _mx_bytes(N, K, MX_TILES)
+    rc = lib().sida_mx_gemm(_gemm_config(groups, N, K, kind, _type(y), 1 if relu else 0)[1], x.data_ptr(), xs, ldx, M,
+                            _flat(codes, groups * n_codes, "uint8", "codes"), _flat(scales, groups * n_scales, "uint8", "scales"),
+                            None if offsets is None else _flat(offsets, 1, "int32", "offsets"), y.data_ptr(), ldy, _stream(stream))
     if rc:
         raise SidaError(rc, "sida_mx_gemm")
 
@@ -262,31 +287,31 @@ def route_workspace_bytes(cfg: SidaRouteConfig, T: int) -> int:
 
 def _route_args(logits, ids, counts, mask, normalize):
     T, E, ld = _rows(logits, "logits")
-    _need(ids.dim() == 2 and ids.shape[0] == T, f"ids: [{T}, experts per token] are needed")
-    cfg = SidaRouteConfig(E, ids.shape[1], _type(logits), 1 if normalize else 0)
-    return (cfg, T, ld, 0 if mask is None else _flat(mask, T, "torch.bool torch.uint8", "mask"),
-            _flat(ids, ids.numel(), "torch.int32", "ids"), _flat(counts, E, "torch.int32", "counts"))
+    if ids.dim() != 2 or ids.shape[0] != T:
+        raise ValueError(f"ids: [{T}, experts per token] are needed")
+    k = ids.shape[1]
+    return (_route_config(E, k, _type(logits), 1 if normalize else 0)[1], T, k, ld, None if mask is None else _flat(mask, T, "bool", "mask"),
+            _flat(ids, T * k, "int32", "ids"), _flat(counts, E, "int32", "counts"))
 
 
 def route(logits, ids, gates, counts, loss, workspace, stream, mask=None, normalize=False):
-    """logits: bf16 or fp32 [T, E]; ids: int32 [T, k]; gates: fp32 [T, k]; counts: int32 [E]; loss: fp32, one value; workspace:
+    """logits: bf16 or fp32 [T, E]; ids: int32 [T, k]; gates: fp32 [T, k]; counts: int32 [E]; loss: fp32, one value; workspace: uint8,
     route_workspace_bytes of it; mask: bool or uint8 [T] or None."""
-    cfg, T, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
-    rc = lib().sida_route(C.byref(cfg), logits.data_ptr(), ld, T, m, i, _flat(gates, ids.numel(), "torch.float32", "gates"), c,
-                          _flat(loss, 1, "torch.float32", "loss"), workspace.data_ptr(),
-                          workspace.numel() * workspace.element_size(), _stream(stream))
+    cfg, T, k, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
+    rc = lib().sida_route(cfg, logits.data_ptr(), ld, T, m, i, _flat(gates, T * k, "fp32", "gates"), c, _flat(loss, 1, "fp32", "loss"),
+                          _flat(workspace, 0, "uint8", "workspace"), workspace.numel(), _stream(stream))
     if rc:
         raise SidaError(rc, "sida_route")
 
 
 def route_backward(logits, ids, counts, d_logits, stream, d_gates=None, d_loss=None, mask=None, normalize=False):
     """d_logits: as logits; d_gates: fp32 [T, k] or None; d_loss: fp32, one value, or None."""
-    cfg, T, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
-    _need(d_logits.shape == logits.shape and d_logits.dtype == logits.dtype, "d_logits: shape and type of the logits are needed")
-    rc = lib().sida_route_backward(C.byref(cfg), logits.data_ptr(), ld, T, m, i, c,
-                                   0 if d_gates is None else _flat(d_gates, ids.numel(), "torch.float32", "d_gates"),
-                                   0 if d_loss is None else _flat(d_loss, 1, "torch.float32", "d_loss"),
-                                   d_logits.data_ptr(), _rows(d_logits, "d_logits")[2], _stream(stream))
+    cfg, T, k, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
+    if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
+        raise ValueError("d_logits: shape and type of the logits are needed")
+    rc = lib().sida_route_backward(cfg, logits.data_ptr(), ld, T, m, i, c, None if d_gates is None else _flat(d_gates, T * k, "fp32", "d_gates"),
+                                   None if d_loss is None else _flat(d_loss, 1, "fp32", "d_loss"), d_logits.data_ptr(),
+                                   _rows(d_logits, "d_logits")[2], _stream(stream))
     if rc:
         raise SidaError(rc, "sida_route_backward")
 

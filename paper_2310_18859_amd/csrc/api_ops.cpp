@@ -85,7 +85,7 @@ int sida_mx_gemm(const sida_mx_gemm_config *c, const void *x_dev, const void *x_
 size_t sida_route_workspace_bytes(const sida_route_config *c, int32_t T)
 {
     if (!route_cfg_ok(c) || !route_rows_ok(c, T, c->E)) return 0;
-    return up((size_t)route_workgroups(T) * c->E * 8, 256);
+    return up(kRouteTailBytes + (size_t)route_workgroups(T) * up(c->E, 4) * 8, 256);
 }
 
 int sida_route(const sida_route_config *c, const void *logits_dev, int64_t ld, int32_t T, const uint8_t *mask_dev, int32_t *ids_dev,

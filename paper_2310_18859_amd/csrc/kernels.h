@@ -148,7 +148,8 @@ struct RouteShape {
     int32_t E, top_k;
     bool fp32, normalize;
 };
-int route_workgroups(int32_t T);   // workgroups of the forward pass: each leaves 8 bytes per expert in the workspace
+constexpr size_t kRouteTailBytes = 128;   // in front of the workgroups' sums in the workspace
+int route_workgroups(int32_t T);   // workgroups of the forward pass: each leaves 8 bytes per expert (a multiple of 4 experts) in the workspace
 int launch_route(const RouteShape &s, const void *logits, int64_t ld, int32_t T, const uint8_t *mask, int32_t *ids, float *gates,
                  int32_t *counts, float *loss, void *ws, hipStream_t st);
 int launch_route_backward(const RouteShape &s, const void *logits, int64_t ld, int32_t T, const uint8_t *mask, const int32_t *ids,

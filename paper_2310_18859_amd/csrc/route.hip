@@ -23,6 +23,9 @@ namespace sida {
 
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
 constexpr int kLanes = 16;                     // lanes per token
 constexpr int kRouteThreads = 1024, kRouteRows = kRouteThreads / kLanes;
 constexpr int kRouteWaves = kRouteThreads / 64;
@@ -135,6 +138,14 @@ struct Row {
 
 __device__ __forceinline__ float power(float v, float m) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); }
 
+// What the second launch's workgroups leave for the last of them; the first launch sets `arrived` to 0.
+struct RouteTail {
+    float term[8];
+    int count[8];
+    int arrived;
+};
+static_assert(sizeof(RouteTail) <= kRouteTailBytes, "workspace");
+
 struct RouteArgs {
     const void *logits;
     const uint8_t *mask;
@@ -144,51 +155,19 @@ struct RouteArgs {
     float *gates;
     int32_t *counts;
     float *loss;
-    float *part_p;               // [workgroups][E]
-    int32_t *part_n;             // [workgroups][E]
+    float *part_p;               // [workgroups][part_ld], part_ld = E filled up to 16 bytes
+    int32_t *part_n;             // the same
+    int part_ld;
+    RouteTail *tail;
     const float *d_gates, *d_loss;
     void *d_logits;
 };
 
-// counts and loss from the workgroups' sums, each expert's in the order of the workgroups within kSlices interleaved parts.
-constexpr int kSlices = kRouteThreads / kMostE;
-__device__ __forceinline__ void finish(const RouteArgs &a, int workgroups, float *p_sum, int *n_sum, float *terms, int *total)
+// The loss from sum_e counts[e] sum_t p[t,e] and the sum of the counts, n k.
+__device__ __forceinline__ float loss_of(const RouteArgs &a, float term, int total)
 {
-    const int tid = threadIdx.x, e = tid % kMostE, slice = tid / kMostE;
-    float p = 0;
-    int n = 0;
-    if (e < a.E) {
-#pragma unroll 8
-        for (int b = slice; b < workgroups; b += kSlices) {
-            p += a.part_p[(size_t)b * a.E + e];
-            n += a.part_n[(size_t)b * a.E + e];
-        }
-    }
-    p_sum[tid] = p;
-    n_sum[tid] = n;
-    if (tid == 0) *total = 0;
-    __syncthreads();
-    if (tid < kMostE) {
-#pragma unroll
-        for (int s = 1; s < kSlices; ++s) {
-            p += p_sum[s * kMostE + tid];
-            n += n_sum[s * kMostE + tid];
-        }
-        if (tid < a.E) {
-            a.counts[tid] = n;
-            atomicAdd(total, n);
-        }
-        terms[tid] = p * (float)n;
-    }
-    __syncthreads();
-    for (int half = kMostE / 2; half > 0; half /= 2) {
-        if (tid < half) terms[tid] += terms[tid + half];
-        __syncthreads();
-    }
-    if (tid == 0) {
-        const float all = (float)*total, tokens = all / a.k;      // all = n k
-        *a.loss = *total ? (float)a.E * (terms[0] / all / tokens) : 0.f;
-    }
+    const float all = (float)total, tokens = all / a.k;
+    return total ? (float)a.E * (term / all / tokens) : 0.f;
 }
 
 template <class T, int VEC, int J>
@@ -197,19 +176,20 @@ __global__ __launch_bounds__(kRouteThreads) void route_rows(const RouteArgs a)
     typedef Row<T, VEC, J> R;
     __shared__ float p_part[kRouteWaves][kMostE];
     __shared__ int n_part[kMostE];
-    __shared__ float p_sum[kRouteThreads];
-    __shared__ int n_sum[kRouteThreads];
-    __shared__ float terms[kMostE];
-    __shared__ int total;
+    __shared__ float sums[8];
     const int tid = threadIdx.x, sub = tid & (kLanes - 1), lane = tid & 63, wave = tid >> 6;
     for (int e = tid; e < kMostE; e += kRouteThreads) n_part[e] = 0;
     __syncthreads();
     float p_acc[R::V];
 #pragma unroll
     for (int i = 0; i < R::V; ++i) p_acc[i] = 0;
-    for (int64_t t = (int64_t)blockIdx.x * kRouteRows + tid / kLanes; t < a.T; t += (int64_t)gridDim.x * kRouteRows) {
-        R r;
-        r.load((const T *)a.logits + t * a.ld, sub, a.E);
+    const int64_t step = (int64_t)gridDim.x * kRouteRows;
+    R next;
+    int64_t t = (int64_t)blockIdx.x * kRouteRows + tid / kLanes;
+    if (t < a.T) next.load((const T *)a.logits + t * a.ld, sub, a.E);
+    for (; t < a.T; t += step) {
+        R r = next;
+        if (t + step < a.T) next.load((const T *)a.logits + (t + step) * a.ld, sub, a.E);   // while this token is dealt with
         const float m = r.largest();
         const bool part = (!a.mask || a.mask[t]) && !r.nothing(m);
         float e[R::V], sum = 0;
@@ -227,7 +207,6 @@ __global__ __launch_bounds__(kRouteThreads) void route_rows(const RouteArgs a)
         // NaN, which no maximum takes.
         int my_id = 0;
         float my_gate = 0, gate_sum = 0, top = m;
-        uint32_t taken = 0;                                  // bit i: place i is chosen
         for (int j = 0; j < a.k; ++j) {
             if (j) top = r.largest();
             int id = INT32_MAX;
@@ -235,6 +214,12 @@ __global__ __launch_bounds__(kRouteThreads) void route_rows(const RouteArgs a)
             for (int i = R::V - 1; i >= 0; --i) id = r.v[i] == top ? R::column(sub, i) : id;
             id = row_min(id);
             if (id >= a.E) {                                 // only NaN are left: the lowest column not chosen yet
+                uint32_t taken = 0;                          // bit i: place i is chosen
+                for (int q = 0; q < j; ++q) {
+                    const int before = __shfl(my_id, (lane & ~(kLanes - 1)) + q);
+#pragma unroll
+                    for (int i = 0; i < R::V; ++i) taken |= R::column(sub, i) == before ? 1u << i : 0u;
+                }
                 id = INT32_MAX;
 #pragma unroll
                 for (int i = R::V - 1; i >= 0; --i)
@@ -249,11 +234,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_rows(const RouteArgs a)
             }
             if (j + 1 < a.k) {
 #pragma unroll
-                for (int i = 0; i < R::V; ++i) {
-                    const bool it = R::column(sub, i) == id;
-                    r.v[i] = it ? NAN : r.v[i];
-                    taken |= it ? 1u << i : 0u;
-                }
+                for (int i = 0; i < R::V; ++i) r.v[i] = R::column(sub, i) == id ? NAN : r.v[i];
             }
         }
         if (sub < a.k) {
@@ -271,26 +252,113 @@ __global__ __launch_bounds__(kRouteThreads) void route_rows(const RouteArgs a)
         if (lane < kLanes) p_part[wave][R::column(sub, i)] = p_acc[i];
     }
     __syncthreads();
+    float p = 0;
+    int n = 0;
     if (tid < a.E) {
-        float p = 0;
 #pragma unroll
         for (int w = 0; w < kRouteWaves; ++w) p += p_part[w][tid];
-        a.part_p[(size_t)blockIdx.x * a.E + tid] = p;
-        a.part_n[(size_t)blockIdx.x * a.E + tid] = n_part[tid];
+        n = n_part[tid];
     }
-    if (gridDim.x == 1) {
-        __syncthreads();                                     // this workgroup's own stores
-        finish(a, 1, p_sum, n_sum, terms, &total);
+    if (gridDim.x > 1) {
+        if (tid < a.E) {
+            a.part_p[(size_t)blockIdx.x * a.part_ld + tid] = p;
+            a.part_n[(size_t)blockIdx.x * a.part_ld + tid] = n;
+        }
+        if (blockIdx.x == 0 && tid == 0) a.tail->arrived = 0;
+        return;
+    }
+    float term = p * (float)n;
+    int total = n;
+    if (tid < kMostE) {
+        if (tid < a.E) a.counts[tid] = n;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            term += __shfl_xor(term, d);
+            total += __shfl_xor(total, d);
+        }
+        if (lane == 0) {
+            sums[wave] = term;
+            sums[4 + wave] = __builtin_bit_cast(float, total);
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        total = 0;
+        for (int w = 0; w < 4; ++w) total += __builtin_bit_cast(int, sums[4 + w]);
+        *a.loss = loss_of(a, sums[0] + sums[1] + (sums[2] + sums[3]), total);
     }
 }
 
-__global__ __launch_bounds__(kRouteThreads) void route_finish(const RouteArgs a, int workgroups)
+// Adds the workgroups' sums.  A workgroup takes 32 experts, 8 threads with 16-byte loads to a row of sums: they were written through other
+// XCDs' caches, and one compute unit alone would wait 9.4 us for the 512 KiB of 256 experts (4.7 us this way).  The
+// workgroup that is the last to arrive, whichever it is, adds the eight terms of the loss in their order.
+constexpr int kFinishE = 32, kFinishThreads = 512, kFinishSlices = kFinishThreads / (kFinishE / 4), kFinishLoads = kRouteBlocks / kFinishSlices;
+__global__ __launch_bounds__(kFinishThreads) void route_finish(const RouteArgs a, int workgroups)
 {
-    __shared__ float p_sum[kRouteThreads];
-    __shared__ int n_sum[kRouteThreads];
-    __shared__ float terms[kMostE];
-    __shared__ int total;
-    finish(a, workgroups, p_sum, n_sum, terms, &total);
+    __shared__ f32x4 p_part[kFinishSlices][kFinishE / 4];
+    __shared__ i32x4 n_part[kFinishSlices][kFinishE / 4];
+    __shared__ float p_sum[kFinishThreads / kFinishE][kFinishE];
+    __shared__ int n_sum[kFinishThreads / kFinishE][kFinishE];
+    const int tid = threadIdx.x, c4 = tid % (kFinishE / 4), slice = tid / (kFinishE / 4), from = blockIdx.x * kFinishE + c4 * 4;
+    f32x4 p[kFinishLoads];
+    i32x4 n[kFinishLoads];
+#pragma unroll
+    for (int i = 0; i < kFinishLoads; ++i) {
+        const int b = i * kFinishSlices + slice;
+        const bool in = b < workgroups && from < a.part_ld;
+        p[i] = in ? *reinterpret_cast<const f32x4 *>(a.part_p + (size_t)b * a.part_ld + from) : f32x4{0, 0, 0, 0};
+        n[i] = in ? *reinterpret_cast<const i32x4 *>(a.part_n + (size_t)b * a.part_ld + from) : i32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 1; i < kFinishLoads; ++i) {
+        p[0] += p[i];
+        n[0] += n[i];
+    }
+    p_part[slice][c4] = p[0];
+    n_part[slice][c4] = n[0];
+    __syncthreads();
+    constexpr int kParts = kFinishThreads / kFinishE, kPer = kFinishSlices / kParts;
+    const int mine = tid % kFinishE, part = tid / kFinishE;
+    float sum = 0;
+    int count = 0;
+#pragma unroll
+    for (int s = 0; s < kPer; ++s) {
+        sum += p_part[part * kPer + s][mine / 4][mine % 4];
+        count += n_part[part * kPer + s][mine / 4][mine % 4];
+    }
+    p_sum[part][mine] = sum;
+    n_sum[part][mine] = count;
+    __syncthreads();
+    if (tid >= 64) return;
+    sum = 0;
+    count = 0;
+    const int e = blockIdx.x * kFinishE + tid;
+    if (tid < kFinishE && e < a.E) {
+#pragma unroll
+        for (int s = 0; s < kParts; ++s) {
+            sum += p_sum[s][tid];
+            count += n_sum[s][tid];
+        }
+        a.counts[e] = count;
+    }
+    float term = sum * (float)count;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        term += __shfl_xor(term, d);
+        count += __shfl_xor(count, d);
+    }
+    if (tid) return;
+    RouteTail *t = a.tail;
+    __hip_atomic_store(&t->term[blockIdx.x], term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&t->count[blockIdx.x], count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__hip_atomic_fetch_add(&t->arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 != (int)gridDim.x) return;
+    term = 0;
+    count = 0;
+    for (int i = 0; i < (int)gridDim.x; ++i) {
+        term += __hip_atomic_load(&t->term[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        count += __hip_atomic_load(&t->count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    *a.loss = loss_of(a, term, count);
 }
 
 constexpr int kBackThreads = 256, kBackRows = kBackThreads / kLanes;
@@ -371,7 +439,7 @@ int launch_forward(const RouteArgs &a, hipStream_t st)
     route_rows<T, VEC, J><<<grid, kRouteThreads, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && grid > 1) {
-        route_finish<<<1, kRouteThreads, 0, st>>>(a, grid);
+        route_finish<<<(a.E + kFinishE - 1) / kFinishE, kFinishThreads, 0, st>>>(a, grid);
         e = hipGetLastError();
     }
     return (int)e;
@@ -436,8 +504,10 @@ int launch_route(const RouteShape &s, const void *logits, int64_t ld, int32_t T,
     RouteArgs a{};
     a.logits = logits, a.ld = ld, a.T = T, a.E = s.E, a.k = s.top_k, a.normalize = s.normalize, a.mask = mask;
     a.ids = ids, a.gates = gates, a.counts = counts, a.loss = loss;
-    a.part_p = (float *)ws;
-    a.part_n = (int32_t *)(a.part_p + (size_t)route_workgroups(T) * s.E);
+    a.tail = (RouteTail *)ws;
+    a.part_p = (float *)((char *)ws + kRouteTailBytes);
+    a.part_ld = (s.E + 3) / 4 * 4;
+    a.part_n = (int32_t *)(a.part_p + (size_t)route_workgroups(T) * a.part_ld);
     return s.fp32 ? forward_typed<float>(a, st) : forward_typed<__bf16>(a, st);
 }
 
