@@ -4,6 +4,7 @@
 #include <cstddef>
 #include <cstdint>
 #include <type_traits>
+#include <utility>
 
 #include "kernels.h"
 
@@ -60,12 +61,14 @@ __device__ __forceinline__ Placed place(const MxArgs &a, int n_tiles)
     int tiles = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) tiles += (max(0, at[i + 1] - at[i]) + BM - 1) / BM;
+    // Sum over this and all lower lanes: in rows of 16 lanes, then row 0's and 2's last lane into rows 1 and 3, lane 31's into the upper half.
     int before = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int v = __shfl_up(before, d);
-        if (lane >= d) before += v;
-    }
+    before += __builtin_amdgcn_update_dpp(0, before, 0x111, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x112, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x114, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x118, 0xf, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x142, 0xa, 0xf, false);
+    before += __builtin_amdgcn_update_dpp(0, before, 0x143, 0xc, 0xf, false);
     const int id = tile_of(__builtin_amdgcn_readlane(before, 63));
     if (id < 0) return Placed{0, 0, 0, 0};
     const int mt = id / n_tiles;
@@ -98,6 +101,12 @@ __device__ __forceinline__ bf16x8 decode(uint32_t c, float s)
 __device__ __forceinline__ i32x8 wide(i32x4 v) { return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }   // 4-bit operands fill half of the registers
 __device__ __forceinline__ float relu_of(float v) { return v <= 0.f ? 0.f : v; }   // NaN stays
 
+template <class F, int... I>
+__device__ __forceinline__ void each(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
+
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
@@ -119,31 +128,34 @@ __device__ __forceinline__ void load_word_to_lds(__amdgpu_buffer_rsrc_t r, uint3
 // Lane offset of a load that asks for nothing: past every descriptor here (128 rows less than 2^25 bytes apart).
 constexpr uint32_t kNowhere = 0xffffff00u;
 
+constexpr int kAhead = 1;
 constexpr int kWaves = 4;
 constexpr int kStageRow = 128;                 // bytes of a token row per stage: 64 values in bf16, 256 in 4 bits
 
-// A workgroup of four wavefronts: 32 MI tokens x 128 NS columns; wavefront w owns NS stripes of 32 columns and all tokens.
+// A tile of up to 32 MI tokens x 128 NS columns by a workgroup of four wavefronts; wavefront w owns NS stripes of 32 columns and all
+// tokens.  Token rows are loaded NB stages ahead of their use and weights WB.
 template <bool X4, int MI, int NS, int NB, int WB, class Y>
-__global__ __launch_bounds__(kWaves * 64, MI == 4 ? 2 : MI == 2 ? (X4 ? 3 : 4) : X4 ? 3 : 5) void mx_gemm_tiles(const MxArgs a)
+struct TileShape {
+    static constexpr int kStage = MI * 32 * kStageRow + (X4 ? 1024 : 0);   // token rows, and their scales
+    static constexpr int kRing = (NB + 1) * kStage;
+    static constexpr int kTurnCols = sizeof(Y) == 2 ? NS * 32 : 32;        // columns that go through LDS together
+    static constexpr int kTurnPitch = kTurnCols * (int)sizeof(Y) + 16;
+    static constexpr int kTurn = kWaves * 32 * kTurnPitch;
+    static constexpr int kLds = kRing > kTurn ? kRing : kTurn;
+};
+template <bool X4, int MI, int NS, int NB, int WB, class Y>
+__device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, char *lds)
 {
-    constexpr int BM = 32 * MI, BN = 32 * NS * kWaves;
-    constexpr int kStage = BM * kStageRow + (X4 ? 1024 : 0);   // token rows, and their scales
-    constexpr int kRing = (NB + 1) * kStage;
-    constexpr int kTurnCols = sizeof(Y) == 2 ? NS * 32 : 32;   // columns that go through LDS together
-    constexpr int kTurnPitch = kTurnCols * (int)sizeof(Y) + 16;
-    constexpr int kTurn = kWaves * 32 * kTurnPitch;
+    typedef TileShape<X4, MI, NS, NB, WB, Y> Shape;
+    constexpr int BM = 32 * MI, kStage = Shape::kStage, kTurnCols = Shape::kTurnCols, kTurnPitch = Shape::kTurnPitch;
     constexpr int WQ = X4 ? 4 : 1;                             // weight fragments per stripe and stage
     // After a stage's token loads at least the token loads of NB - 1 later stages and WB stages of weights are asked for
     // before it is used; the waits for the weights themselves are the compiler's.
     constexpr int kLater = (NB - 1) * (MI + (X4 ? 1 : 0)) + WB * NS * (WQ + 1);
     static_assert(kLater <= 63 && NB % WB == 0, "vmcnt range");
-    __shared__ __attribute__((aligned(1024))) char lds[kRing > kTurn ? kRing : kTurn];
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n_tiles = (a.N + BN - 1) / BN;
-    const Placed at = place<BM>(a, n_tiles);
-    if (at.rows == 0) return;
     const int stripe0 = at.nt * (NS * kWaves) + wv * NS, stripes = (a.N + 31) / 32;
     const int chunks = (a.K + 63) / 64, groups = (a.K + 255) / 256;
     const int row_bytes = X4 ? a.K / 2 : a.K * 2;
@@ -209,42 +221,42 @@ __global__ __launch_bounds__(kWaves * 64, MI == 4 ? 2 : MI == 2 ? (X4 ? 3 : 4) :
         for (int m = 0; m < MI; ++m)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[s][m][r] = 0;
-    const int live = (at.rows + 31) / 32;
     int frag_off[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) frag_off[q] = (lane & 31) * kStageRow + (((X4 ? 2 * q + half : half * 4 + q) ^ ((lane & 31) >> 1 & 7)) * 16);
-    auto multiply = [&](auto blocks, int b, int slot) {
-        constexpr int L = decltype(blocks)::value;
+    auto multiply = [&](int b, int slot) {
         const char *src = lds + slot * kStage;
-        uint32_t xs[L];
+        uint32_t xs[MI];
         if constexpr (X4)
 #pragma unroll
-            for (int m = 0; m < L; ++m) {
+            for (int m = 0; m < MI; ++m) {
                 const u32x2 both = *reinterpret_cast<const u32x2 *>(src + BM * kStageRow + (m * 32 + (lane & 31)) * 8);
                 xs[m] = __builtin_amdgcn_perm(both[1], both[0], half ? 0x07050301u : 0x06040200u);
             }
+        // Token fragments are read kAhead products' pairs ahead; the compiler would read them where they are used.
+        constexpr int kSteps = 4 * MI, kHeld = kAhead + 1;
+        i32x4 held[kHeld];
+        auto read = [&](int k) { held[k % kHeld] = *reinterpret_cast<const i32x4 *>(src + (k % MI) * 32 * kStageRow + frag_off[k / MI]); };
+#pragma unroll
+        for (int k = 0; k < kAhead && k < kSteps; ++k) read(k);
+        bf16x8 v[NS];
         auto step = [&](auto place) {
-            constexpr int q = decltype(place)::value;
-            bf16x8 v[NS];
-            if constexpr (!X4)
+            constexpr int k = decltype(place)::value, q = k / MI, m = k % MI;
+            if constexpr (k + kAhead < kSteps) read(k + kAhead);
+            if constexpr (!X4 && m == 0)
 #pragma unroll
                 for (int s = 0; s < NS; ++s) v[s] = decode(w[b][s][0][q], __builtin_bit_cast(float, ws[b][s] << 23));
+            const i32x4 x = held[k % kHeld];
 #pragma unroll
-            for (int m = 0; m < L; ++m) {
-                const i32x4 x = *reinterpret_cast<const i32x4 *>(src + m * 32 * kStageRow + frag_off[q]);
-#pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    if constexpr (X4)
-                        acc[s][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(w[b][s][q]), wide(x), acc[s][m], 4, 4, q, ws[b][s], q, xs[m]);
-                    else
-                        acc[s][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[s], __builtin_bit_cast(bf16x8, x), acc[s][m], 0, 0, 0);
-                }
+            for (int s = 0; s < NS; ++s) {
+                if constexpr (X4)
+                    acc[s][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(w[b][s][q]), wide(x), acc[s][m], 4, 4, q, ws[b][s], q, xs[m]);
+                else
+                    acc[s][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[s], __builtin_bit_cast(bf16x8, x), acc[s][m], 0, 0, 0);
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
-        step(std::integral_constant<int, 0>());
-        step(std::integral_constant<int, 1>());
-        step(std::integral_constant<int, 2>());
-        step(std::integral_constant<int, 3>());
+        each(step, std::make_integer_sequence<int, kSteps>());
     };
 
     // In front of the loop in the loop's order, so that the compiler's waits for the weights are as loose there.
@@ -254,39 +266,31 @@ __global__ __launch_bounds__(kWaves * 64, MI == 4 ? 2 : MI == 2 ? (X4 ? 3 : 4) :
         if (i + WB >= 0) load_weights((i + NB) % WB, i + WB);
         __builtin_amdgcn_sched_barrier(0);
     }
-    // All stages, for the token blocks that the tile has: straight code for each number of them.
-    auto sum = [&](auto blocks) {
-        int t = 0, slot = 0;
-        auto next = [](int v) { return v == NB ? 0 : v + 1; };
-        for (; t + NB <= stages; t += NB) {
+    int t = 0, slot = 0;
+    for (; t + NB <= stages; t += NB) {
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                wait_loads<kLater>();
-                __builtin_amdgcn_s_barrier();
-                __builtin_amdgcn_sched_barrier(0);
-                load_tokens(t + i + NB, slot ? slot - 1 : NB);
-                multiply(blocks, i % WB, slot);
-                __builtin_amdgcn_sched_barrier(0);             // loads any earlier would need registers of their own
-                load_weights(i % WB, t + i + WB);
-                slot = next(slot);
-            }
+        for (int i = 0; i < NB; ++i) {
+            wait_loads<kLater>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            load_tokens(t + i + NB, slot ? slot - 1 : NB);
+            multiply(i % WB, slot);
+            __builtin_amdgcn_sched_barrier(0);                 // loads any earlier would need registers of their own
+            load_weights(i % WB, t + i + WB);
+            slot = slot == NB ? 0 : slot + 1;
         }
-        wait_loads<0>();
-        __builtin_amdgcn_s_barrier();
-        if constexpr (NB > 1) {
+    }
+    wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    if constexpr (NB > 1) {                                    // what is left of the stages has been loaded (weights: WB of them)
 #pragma unroll
-            for (int i = 0; i < NB - 1; ++i) {
-                if (t + i >= stages) break;
-                multiply(blocks, i % WB, slot);
-                if (WB < NB) load_weights(i % WB, t + i + WB);
-                slot = next(slot);
-            }
+        for (int i = 0; i < NB - 1; ++i) {
+            if (t + i >= stages) break;
+            multiply(i % WB, slot);
+            if (WB < NB - 1) load_weights(i % WB, t + i + WB);
+            slot = slot == NB ? 0 : slot + 1;
         }
-    };
-    if (live == 1) sum(std::integral_constant<int, 1>());
-    else if (MI == 2 || live == 2) sum(std::integral_constant<int, MI < 2 ? 1 : 2>());
-    else if (live == 3) sum(std::integral_constant<int, MI < 3 ? 1 : 3>());
-    else sum(std::integral_constant<int, MI>());
+    }
     __builtin_amdgcn_s_barrier();
 
     // Results.  A lane holds four times four consecutive columns of one token.
@@ -297,7 +301,6 @@ __global__ __launch_bounds__(kWaves * 64, MI == 4 ? 2 : MI == 2 ? (X4 ? 3 : 4) :
         constexpr int kLanes = kTurnCols * (int)sizeof(Y) / 16; // lanes per row piece
 #pragma unroll
         for (int m = 0; m < MI; ++m) {
-            if (m >= live) break;
 #pragma unroll
             for (int s0 = 0; s0 < NS; s0 += kPer) {
 #pragma unroll
@@ -319,7 +322,7 @@ __global__ __launch_bounds__(kWaves * 64, MI == 4 ? 2 : MI == 2 ? (X4 ? 3 : 4) :
                     const int r = i * (64 / kLanes) + lane / kLanes, c = lane % kLanes * (16 / (int)sizeof(Y));
                     const i32x4 v = *reinterpret_cast<const i32x4 *>(turn + r * kTurnPitch + c * (int)sizeof(Y));
                     const int col = (stripe0 + s0) * 32 + c;
-                    if (m * 32 + r < at.rows && col < a.N) *reinterpret_cast<i32x4 *>(y + (int64_t)(m * 32 + r) * a.ldy + col) = v;
+                    if (m * 32 + r < at.rows && col < a.N) __builtin_nontemporal_store(v, reinterpret_cast<i32x4 *>(y + (int64_t)(m * 32 + r) * a.ldy + col));
                 }
                 __builtin_amdgcn_wave_barrier();
             }
@@ -339,6 +342,20 @@ __global__ __launch_bounds__(kWaves * 64, MI == 4 ? 2 : MI == 2 ? (X4 ? 3 : 4) :
                 }
         }
     }
+}
+
+// A kernel for tiles of up to 32 MI tokens; each number of 32-token blocks has a way of its own through it, with registers and loads
+// for that many blocks and no more.
+template <bool X4, int MI, int NS, int NB, int WB, int OCC, class Y>
+__global__ __launch_bounds__(kWaves * 64, OCC) void mx_gemm_tiles(const MxArgs a)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[TileShape<X4, MI, NS, NB, WB, Y>::kLds];
+    const Placed at = place<32 * MI>(a, (a.N + 128 * NS - 1) / (128 * NS));
+    if (at.rows == 0) return;
+    if (MI > 1 && at.rows <= 32) return take_tile<X4, 1, NS, NB, WB, Y>(a, at, lds);
+    if (MI > 2 && at.rows <= 64) return take_tile<X4, 2, NS, NB, WB, Y>(a, at, lds);
+    if (MI > 3 && at.rows <= 96) return take_tile<X4, 3, NS, NB, WB, Y>(a, at, lds);
+    take_tile<X4, MI, NS, NB, WB, Y>(a, at, lds);
 }
 
 // Few rows, few tiles: a single token's product is a few hundred kilobytes for the whole chip, and what counts is how long the
@@ -403,12 +420,12 @@ __global__ __launch_bounds__(kSplit * 64, 4) void mx_gemm_split(const MxArgs a)
     if (token < at.rows && col < a.N) ((Y *)a.y)[(int64_t)(at.row0 + token) * a.ldy + col] = (Y)(a.relu ? relu_of(sum) : sum);
 }
 
-template <bool X4, int MI, int NS, int NB, int WB, class Y>
+template <bool X4, int MI, int NS, int NB, int WB, int OCC, class Y>
 int launch_shape(const MxArgs &a, hipStream_t st)
 {
     constexpr int BM = 32 * MI, BN = 32 * NS * kWaves;
     const int64_t tiles = a.M / BM + (a.groups < a.M ? a.groups : a.M), grid = tiles * ((a.N + BN - 1) / BN);
-    mx_gemm_tiles<X4, MI, NS, NB, WB, Y><<<(uint32_t)((grid + 7) / 8 * 8), kWaves * 64, 0, st>>>(a);
+    mx_gemm_tiles<X4, MI, NS, NB, WB, OCC, Y><<<(uint32_t)((grid + 7) / 8 * 8), kWaves * 64, 0, st>>>(a);
     return (int)hipGetLastError();
 }
 
@@ -424,10 +441,17 @@ int launch_typed(const MxArgs &a, hipStream_t st)
         mx_gemm_split<X4, Y><<<(uint32_t)((few + 7) / 8 * 8), kSplit * 64, 0, st>>>(a);
         return (int)hipGetLastError();
     }
-    const int mean = a.M / a.groups;
-    if (X4 && mean > 64) return launch_shape<X4, 4, 2, 2, 1, Y>(a, st);
-    if (mean > 32) return launch_shape<X4, 2, 2, 2, X4 ? 1 : 2, Y>(a, st);
-    return launch_shape<X4, 1, 1, X4 ? 2 : 4, X4 ? 2 : 4, Y>(a, st);
+    // Tile height and width, by how many rows a group has on average and how many tiles of 64 x 256 there would be (256 of them, four to a
+    // compute unit, are a round).  us, 32 x 128 against 64 x 256, 64 groups, K x N: tokens in bf16, 48 a group, 768 x 3072 27.3 / 22.6, 64 a group,
+    // 1024 x 1024 16.6 / 18.0, 3072 x 768 29.8 / 41.6, 128 a group 48.9 / 44.8; in 4 bits, 24 a group, 768 x 3072 16.2 / 15.7, 32 a
+    // group, 4096 x 1024, Zipf sizes, 28.3 / 29.7, 64 a group 34.2 / 30.8.
+    const int64_t mean = a.M / a.groups, wide = (a.M / 64 + a.groups / 2) * (int64_t)((a.N + 255) / 256);
+    if (X4 ? mean <= 16 || wide < 320 : mean <= 32 || wide < 480) return launch_shape<X4, 1, 1, X4 ? 2 : 4, X4 ? 2 : 4, X4 ? 5 : 6, Y>(a, st);
+    // 128 x 256 for long rows in 4 bits: 256 tokens for each of 128 groups, 4096 x 1024, 109 us against 122; with rows of 768 three stages
+    // are a tile's whole sum, and two workgroups to a compute unit too few (256 a group, 64 groups, 43.0 against 38.1).
+    if constexpr (X4)
+        if (a.K >= 2048 && mean >= 192) return launch_shape<X4, 4, 2, 2, 1, 2, Y>(a, st);
+    return launch_shape<X4, 2, 2, 2, X4 ? 1 : 2, 4, Y>(a, st);
 }
 
 }  // namespace
