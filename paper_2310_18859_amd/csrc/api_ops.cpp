@@ -73,6 +73,7 @@ int sida_mx_gemm(const sida_mx_gemm_config *c, const void *x_dev, const void *x_
     const bool x4 = c->x_type == SIDA_MXFP4, y32 = c->y_type == SIDA_FP32;
     if (M < 0 || M > 1 << 24 || ldx < c->K || ldx >= kMostPitch || ldy < c->N || ldy >= kMostPitch) return SIDA_EINVAL;
     if (x4 ? ldx != c->K : ldx % 8 != 0) return SIDA_EINVAL;
+    if ((int64_t)M * c->N > (int64_t)1 << 35) return SIDA_EINVAL;      // tiles of 32 x 128 at least: a launch's workgroups
     if (M == 0) return SIDA_OK;
     if (!x_dev || !codes_dev || !scales_dev || !y_dev || (x4 && !x_scales_dev) || (!offsets_dev && c->groups != 1)) return SIDA_EINVAL;
     if (!aligned(x_dev, 16) || !aligned(codes_dev, 16) || !aligned(scales_dev, 4) || !aligned(y_dev, y32 ? 4 : 2) || !aligned(offsets_dev, 4) ||

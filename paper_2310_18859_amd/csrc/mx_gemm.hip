@@ -128,7 +128,6 @@ __device__ __forceinline__ void load_word_to_lds(__amdgpu_buffer_rsrc_t r, uint3
 // Lane offset of a load that asks for nothing: past every descriptor here (128 rows less than 2^25 bytes apart).
 constexpr uint32_t kNowhere = 0xffffff00u;
 
-constexpr int kAhead = 1;
 constexpr int kWaves = 4;
 constexpr int kStageRow = 128;                 // bytes of a token row per stage: 64 values in bf16, 256 in 4 bits
 
@@ -233,8 +232,9 @@ __device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, cha
                 const u32x2 both = *reinterpret_cast<const u32x2 *>(src + BM * kStageRow + (m * 32 + (lane & 31)) * 8);
                 xs[m] = __builtin_amdgcn_perm(both[1], both[0], half ? 0x07050301u : 0x06040200u);
             }
-        // Token fragments are read kAhead products' pairs ahead; the compiler would read them where they are used.
-        constexpr int kSteps = 4 * MI, kHeld = kAhead + 1;
+        // Token fragments are read one step ahead of their products (the compiler would read them where they are used), where the registers
+        // allow it; further ahead gains nothing (16384 x 4096 x 4096: 415, 404, 403, 405 us for 0 to 3 steps).
+        constexpr int kSteps = 4 * MI, kAhead = X4 && MI == 2 ? 0 : 1, kHeld = kAhead + 1;
         i32x4 held[kHeld];
         auto read = [&](int k) { held[k % kHeld] = *reinterpret_cast<const i32x4 *>(src + (k % MI) * 32 * kStageRow + frag_off[k / MI]); };
 #pragma unroll

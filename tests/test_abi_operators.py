@@ -39,7 +39,7 @@ def gemm(groups=2, N=64, K=64, x_type=sm.BF16, y_type=sm.BF16, relu=0, x=P, xs=0
 
 @pytest.mark.parametrize("bad", [dict(cfg=False), dict(groups=0), dict(groups=257), dict(N=0), dict(N=65537, ldy=65537), dict(K=0), dict(K=40), dict(K=16416, ldx=16416),
                                  dict(x_type=sm.FP32), dict(x_type=3), dict(y_type=sm.MXFP4), dict(x=0), dict(codes=0), dict(scales=0), dict(y=0),
-                                 dict(offsets=0), dict(M=-1), dict(M=(1 << 24) + 1), dict(ldx=56), dict(ldx=68), dict(ldx=1 << 24), dict(ldy=63),
+                                 dict(offsets=0), dict(M=-1), dict(M=(1 << 24) + 1), dict(M=1 << 24, N=4096, ldy=4096), dict(ldx=56), dict(ldx=68), dict(ldx=1 << 24), dict(ldy=63),
                                  dict(ldy=1 << 24), dict(x=P + 8), dict(codes=P + 4), dict(scales=P + 2), dict(y=P + 1), dict(y=P + 2, y_type=sm.FP32),
                                  dict(offsets=P + 2), dict(x_type=sm.MXFP4), dict(x_type=sm.MXFP4, xs=P + 4), dict(x_type=sm.MXFP4, xs=P, ldx=72)])
 def test_gemm_refuses(bad):
