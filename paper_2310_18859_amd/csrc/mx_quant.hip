@@ -194,11 +194,11 @@ __global__ __launch_bounds__(256) void mx_round_tiles(const T *__restrict__ x, i
         // block j = piece / 4 of this group: 512 bytes of codes per j, 16 per row
         code_tile[(piece / 4) * 128 + r * 4 + piece % 4] = q.codes;
         if (piece % 4 == 0) scale_tile[(piece / 4 % 2) * 128 + r * 4 + piece / 8] = (uint8_t)q.scale;
-        if (live && values) values[row * (cols / 8) + col / 8] = values_of(q);
+        if (live && values) __builtin_nontemporal_store(values_of(q), &values[row * (cols / 8) + col / 8]);
     }
     __syncthreads();
     if (group * 4 + (tid >> 6) < chunks)                      // a chunk of 64 columns is 64 pieces of 16 bytes
-        codes[(stripe * chunks + group * 4) * 64 + tid] = reinterpret_cast<const u32x4 *>(code_tile)[tid];
+        __builtin_nontemporal_store(reinterpret_cast<const u32x4 *>(code_tile)[tid], &codes[(stripe * chunks + group * 4) * 64 + tid]);
     if (tid < 16) scales[(stripe * groups + group) * 16 + tid] = reinterpret_cast<const u32x4 *>(scale_tile)[tid];
 }
 

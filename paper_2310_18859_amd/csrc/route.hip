@@ -112,7 +112,7 @@ struct Row {
                     Vec x;
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) x[i] = (T)v[j * VEC + i];
-                    *reinterpret_cast<Vec *>(row + c) = x;
+                    __builtin_nontemporal_store(x, reinterpret_cast<Vec *>(row + c));
                 }
             }
         }
