@@ -33,6 +33,11 @@ struct MxArgs {
     int relu, whole_lines;       // whole_lines: rows of y start on 16-byte boundaries, N is a multiple of 32
 };
 
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
+}
+
 // Which tile a workgroup takes.  Token tiles are counted group by group (BM rows each, a group's last one less), and each has
 // n_tiles column tiles.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles there are, one after the other, so
 // that a token tile's rows and a group's matrix are fetched into one L2.  Every wavefront finds its tile by itself, four groups to
@@ -55,9 +60,13 @@ __device__ __forceinline__ Placed place(const MxArgs &a, int n_tiles)
         const int row0 = id / n_tiles * BM;
         return Placed{0, row0, min(BM, a.M - row0), id % n_tiles};
     }
+    // Entries past the last one come as zeros: groups without rows.
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.offsets, (uint32_t)(a.groups + 1) * 4);
+    const i32x4 mine = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, 0, 0));
+    const int next = __builtin_amdgcn_raw_buffer_load_b32(r, lane * 16 + 16, 0, 0);
     int at[5];
 #pragma unroll
-    for (int i = 0; i < 5; ++i) at[i] = max(0, min(a.M, a.offsets[min(lane * 4 + i, a.groups)]));
+    for (int i = 0; i < 5; ++i) at[i] = max(0, min(a.M, i < 4 ? mine[i] : next));
     int tiles = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) tiles += (max(0, at[i + 1] - at[i]) + BM - 1) / BM;
@@ -112,10 +121,6 @@ __device__ __forceinline__ void wait_loads()
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, uint32_t bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
-}
 // 16 or 4 bytes per lane straight into LDS: lane i's land at dst + 16 * i or 4 * i.
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t offset, void *dst)
 {
@@ -150,7 +155,7 @@ __device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, cha
     constexpr int WQ = X4 ? 4 : 1;                             // weight fragments per stripe and stage
     // After a stage's token loads at least the token loads of NB - 1 later stages and WB stages of weights are asked for
     // before it is used; the waits for the weights themselves are the compiler's.
-    constexpr int kLater = (NB - 1) * (MI + (X4 ? 1 : 0)) + WB * NS * (WQ + 1);
+    constexpr int kLater = (NB - 1) * (MI + (X4 ? 1 : 0)) + WB * NS * (WQ + (X4 ? 1 : 0));
     static_assert(kLater <= 63 && NB % WB == 0, "vmcnt range");
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -198,19 +203,25 @@ __device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, cha
         s_bytes[s] = in ? groups * 256 : 0;
     }
     i32x4 w[WB][NS][WQ];
-    uint32_t ws[WB][NS];
-    auto load_weights = [&](int b, int stage) {
-        const bool in = stage < stages;
-        const int w_from = in ? stage * (WQ * 1024) : 0, s_from = in ? (X4 ? stage * 256 : (stage >> 2) * 256 + (stage & 3)) : 0;
+    // Powers of two: a lane's four bytes are those of 256 columns, in 4 bits a stage, in bf16 four stages (asked for that far ahead).
+    uint32_t ws[X4 ? WB : 1][NS], ws_next[NS];
+    auto load_scales = [&](uint32_t (&to)[NS], int from256) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            const __amdgpu_buffer_rsrc_t r = make_rsrc(w_at[s] + w_from, in && w_bytes[s] ? w_bytes[s] - w_from : 0);
-            const __amdgpu_buffer_rsrc_t rs = make_rsrc(s_at[s] + s_from, in && s_bytes[s] ? s_bytes[s] - s_from : 0);
+            const bool in = from256 < groups && s_bytes[s];
+            to[s] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(s_at[s] + (in ? from256 * 256 : 0), in ? s_bytes[s] - from256 * 256 : 0), lane * 4, 0, 0);
+        }
+    };
+    auto load_weights = [&](int b, int stage) {
+        const bool in = stage < stages;
+        const int from = in ? stage * (WQ * 1024) : 0;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const __amdgpu_buffer_rsrc_t r = make_rsrc(w_at[s] + from, in && w_bytes[s] ? w_bytes[s] - from : 0);
 #pragma unroll
             for (int q = 0; q < WQ; ++q) w[b][s][q] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16 + q * 1024, 0, 0));
-            if (X4) ws[b][s] = __builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, 0, 0);
-            else ws[b][s] = __builtin_amdgcn_raw_buffer_load_b8(rs, lane * 4, 0, 0);
         }
+        if constexpr (X4) load_scales(ws[b], stage);
     };
 
     f32x16 acc[NS][MI];
@@ -223,7 +234,7 @@ __device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, cha
     int frag_off[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) frag_off[q] = (lane & 31) * kStageRow + (((X4 ? 2 * q + half : half * 4 + q) ^ ((lane & 31) >> 1 & 7)) * 16);
-    auto multiply = [&](int b, int slot) {
+    auto multiply = [&](int b, int slot, int turn) {           // turn: which of a loop turn's stages
         const char *src = lds + slot * kStage;
         uint32_t xs[MI];
         if constexpr (X4)
@@ -245,7 +256,7 @@ __device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, cha
             if constexpr (k + kAhead < kSteps) read(k + kAhead);
             if constexpr (!X4 && m == 0)
 #pragma unroll
-                for (int s = 0; s < NS; ++s) v[s] = decode(w[b][s][0][q], __builtin_bit_cast(float, ws[b][s] << 23));
+                for (int s = 0; s < NS; ++s) v[s] = decode(w[b][s][0][q], __builtin_bit_cast(float, (ws[0][s] >> (turn * 8) & 255u) << 23));
             const i32x4 x = held[k % kHeld];
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
@@ -259,38 +270,45 @@ __device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, cha
         each(step, std::make_integer_sequence<int, kSteps>());
     };
 
-    // In front of the loop in the loop's order, so that the compiler's waits for the weights are as loose there.
+    // In front of the loop in the loop's order, so that the compiler's waits for the weights are as loose there.  A stage's tokens have to
+    // be asked for in front of its weights: kLater counts on it.
+    if constexpr (!X4) load_scales(ws[0], 0);
 #pragma unroll
     for (int i = -NB; i < 0; ++i) {
-        load_tokens(i + NB, i + NB);
-        if (i + WB >= 0) load_weights((i + NB) % WB, i + WB);
         __builtin_amdgcn_sched_barrier(0);
+        load_tokens(i + NB, i + NB);
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + WB >= 0) load_weights((i + NB) % WB, i + WB);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int kTurn = X4 ? WB : 4;                          // stages a turn of the loop
+    static_assert(kTurn % WB == 0, "weight registers");
     int t = 0, slot = 0;
-    for (; t + NB <= stages; t += NB) {
+    auto stage = [&](int i, auto left) {                        // the turn's stage i
+        wait_loads<decltype(left)::value ? 0 : kLater>();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        load_tokens(t + i + NB, slot ? slot - 1 : NB);
+        multiply(i % WB, slot, i);
+        __builtin_amdgcn_sched_barrier(0);                     // loads any earlier would need registers of their own
+        load_weights(i % WB, t + i + WB);
+        if (!X4 && i == 0) load_scales(ws_next, t / 4 + 1);
+        slot = slot == NB ? 0 : slot + 1;
+    };
+    for (; t + kTurn <= stages; t += kTurn) {
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            wait_loads<kLater>();
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
-            load_tokens(t + i + NB, slot ? slot - 1 : NB);
-            multiply(i % WB, slot);
-            __builtin_amdgcn_sched_barrier(0);                 // loads any earlier would need registers of their own
-            load_weights(i % WB, t + i + WB);
-            slot = slot == NB ? 0 : slot + 1;
-        }
-    }
-    wait_loads<0>();
-    __builtin_amdgcn_s_barrier();
-    if constexpr (NB > 1) {                                    // what is left of the stages has been loaded (weights: WB of them)
+        for (int i = 0; i < kTurn; ++i) stage(i, std::false_type());
+        if constexpr (!X4)
 #pragma unroll
-        for (int i = 0; i < NB - 1; ++i) {
-            if (t + i >= stages) break;
-            multiply(i % WB, slot);
-            if (WB < NB - 1) load_weights(i % WB, t + i + WB);
-            slot = slot == NB ? 0 : slot + 1;
-        }
+            for (int s = 0; s < NS; ++s) ws[0][s] = ws_next[s];
     }
+    if constexpr (kTurn > 1)
+#pragma unroll
+        for (int i = 0; i < kTurn - 1; ++i) {                  // What is left of the stages, less than a turn.  Loads whose results nobody
+            if (t + i >= stages) break;                        // takes are not in the program here: nothing is counted on.
+            stage(i, std::true_type());
+        }
+    wait_loads<0>();                                            // the last loads still write LDS
     __builtin_amdgcn_s_barrier();
 
     // Results.  A lane holds four times four consecutive columns of one token.
