@@ -430,8 +430,8 @@ int sida_mx_quantize(const void *x_dev, int32_t x_type, int64_t rows, int32_t co
  *   offsets_dev int32 [groups+1], ascending, 0 .. M.  Values outside are taken as the nearest of 0 and M, a group whose end
  *               is before its start as empty; rows of y that belong to no group keep what they hold (with offsets that do not
                ascend, which of the rows are computed is not defined; no others are touched).  NULL with one group: all rows.
- *   y_dev       y_type SIDA_BF16 or SIDA_FP32: [M, N], rows ldy values apart (ldy >= N), at any address of such a value; where
- *               rows begin on 16-byte boundaries and N is a multiple of 32, results are stored in whole lines.
+ *   y_dev       y_type SIDA_BF16 or SIDA_FP32: [M, N], rows ldy values apart (ldy >= N), at any address of such a value;
+ *               faster where all rows begin and end on 16-byte boundaries, and on 4-byte ones in bf16.
  * Limits: 1 <= groups <= SIDA_MAX_E; K as cols above; 1 <= N <= 65536; 0 <= M <= 2^24, M * N <= 2^35; ldx, ldy < 2^24. */
 typedef struct sida_mx_gemm_config {
     int32_t groups;       /* experts                                       */

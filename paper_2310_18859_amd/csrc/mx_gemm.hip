@@ -30,7 +30,7 @@ struct MxArgs {
     int64_t ldx, ldy;            // values between rows
     int64_t code_bytes, scale_bytes;   // between experts
     int M, N, K, groups;
-    int relu, whole_lines;       // whole_lines: rows of y start on 16-byte boundaries, N is a multiple of 32
+    int relu, unit;              // unit: 16, 4 or 2 bytes that every row of y starts and ends on a multiple of
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, uint32_t bytes)
@@ -109,6 +109,11 @@ __device__ __forceinline__ bf16x8 decode(uint32_t c, float s)
 
 __device__ __forceinline__ i32x8 wide(i32x4 v) { return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }   // 4-bit operands fill half of the registers
 __device__ __forceinline__ float relu_of(float v) { return v <= 0.f ? 0.f : v; }   // NaN stays
+
+template <class T>
+struct Of {
+    typedef T type;
+};
 
 template <class F, int... I>
 __device__ __forceinline__ void each(F &&f, std::integer_sequence<int, I...>)
@@ -311,53 +316,52 @@ __device__ __forceinline__ void take_tile(const MxArgs &a, const Placed &at, cha
     wait_loads<0>();                                            // the last loads still write LDS
     __builtin_amdgcn_s_barrier();
 
-    // Results.  A lane holds four times four consecutive columns of one token.
+    // Results.  A lane holds four times four consecutive columns of one token; turned around in LDS, consecutive lanes store consecutive
+    // pieces of a row, 16 bytes each, or as much as the rows' alignment allows (20926 tokens, 320 x 601: 50 us where lanes stored their own
+    // columns one by one, 25 so).
     Y *y = (Y *)a.y + (int64_t)at.row0 * a.ldy;
-    if (a.whole_lines) {
-        char *turn = lds + wv * 32 * kTurnPitch;
-        constexpr int kPer = kTurnCols / 32;                    // stripes per turn
-        constexpr int kLanes = kTurnCols * (int)sizeof(Y) / 16; // lanes per row piece
+    char *turn = lds + wv * 32 * kTurnPitch;
+    constexpr int kPer = kTurnCols / 32;                        // stripes per turn
+    auto put = [&](auto unit, int m, int s0) {
+        typedef typename decltype(unit)::type Unit;
+        constexpr int kOf = (int)(sizeof(Unit) / sizeof(Y)), kLanes = kTurnCols / kOf;   // columns of a piece, pieces of a row
 #pragma unroll
-        for (int m = 0; m < MI; ++m) {
-#pragma unroll
-            for (int s0 = 0; s0 < NS; s0 += kPer) {
-#pragma unroll
-                for (int s = 0; s < kPer; ++s)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        typedef __attribute__((ext_vector_type(4))) Y Y4;
-                        Y4 v;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float e = acc[s0 + s][m][4 * q + j];
-                            v[j] = (Y)(a.relu ? relu_of(e) : e);
-                        }
-                        *reinterpret_cast<Y4 *>(turn + (lane & 31) * kTurnPitch + (s * 32 + q * 8 + half * 4) * (int)sizeof(Y)) = v;
-                    }
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int i = 0; i < 32 * kLanes / 64; ++i) {
-                    const int r = i * (64 / kLanes) + lane / kLanes, c = lane % kLanes * (16 / (int)sizeof(Y));
-                    const i32x4 v = *reinterpret_cast<const i32x4 *>(turn + r * kTurnPitch + c * (int)sizeof(Y));
-                    const int col = (stripe0 + s0) * 32 + c;
-                    if (m * 32 + r < at.rows && col < a.N) __builtin_nontemporal_store(v, reinterpret_cast<i32x4 *>(y + (int64_t)(m * 32 + r) * a.ldy + col));
-                }
-                __builtin_amdgcn_wave_barrier();
-            }
+        for (int i = 0; i < 32 * kLanes / 64; ++i) {
+            const int at_piece = i * 64 + lane, r = at_piece / kLanes, c = at_piece % kLanes * kOf;
+            const Unit v = *reinterpret_cast<const Unit *>(turn + r * kTurnPitch + c * (int)sizeof(Y));
+            const int row = m * 32 + r, col = (stripe0 + s0) * 32 + c;
+            if (row >= at.rows || col >= a.N) continue;
+            Unit *to = reinterpret_cast<Unit *>(y + (int64_t)row * a.ldy + col);
+            if constexpr (sizeof(Unit) == 16) __builtin_nontemporal_store(v, to);        // whole lines, past L2's replacement
+            else *to = v;
         }
-    } else {
+    };
 #pragma unroll
-        for (int m = 0; m < MI; ++m) {
-            const int r = m * 32 + (lane & 31);
-            if (r >= at.rows) continue;
+    for (int m = 0; m < MI; ++m) {
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
+        for (int s0 = 0; s0 < NS; s0 += kPer) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int col = (stripe0 + s) * 32 + 8 * (j / 4) + 4 * half + j % 4;
-                    const float e = acc[s][m][j];
-                    if (col < a.N) y[(int64_t)r * a.ldy + col] = (Y)(a.relu ? relu_of(e) : e);
+            for (int s = 0; s < kPer; ++s)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    typedef __attribute__((ext_vector_type(4))) Y Y4;
+                    Y4 v;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float e = acc[s0 + s][m][4 * q + j];
+                        v[j] = (Y)(a.relu ? relu_of(e) : e);
+                    }
+                    *reinterpret_cast<Y4 *>(turn + (lane & 31) * kTurnPitch + (s * 32 + q * 8 + half * 4) * (int)sizeof(Y)) = v;
                 }
+            __builtin_amdgcn_wave_barrier();
+            if (a.unit == 16) {
+                put(Of<i32x4>(), m, s0);
+            } else if (sizeof(Y) == 4 || a.unit == 4) {
+                put(Of<uint32_t>(), m, s0);
+            } else {
+                put(Of<Y>(), m, s0);
+            }
+            __builtin_amdgcn_wave_barrier();
         }
     }
 }
@@ -485,7 +489,8 @@ int launch_mx_gemm(const MxShape &sh, const void *x, const void *x_scales, int64
     a.scale_bytes = n * ((sh.K + 255) / 256 * 8);
     a.relu = sh.relu;
     const size_t size = sh.y32 ? 4 : 2;
-    a.whole_lines = ((uintptr_t)y | (size_t)ldy * size) % 16 == 0 && sh.N % 32 == 0;
+    const size_t ends = (uintptr_t)y | (size_t)ldy * size | (size_t)sh.N * size;
+    a.unit = ends % 16 == 0 ? 16 : ends % 4 == 0 ? 4 : 2;
     if (sh.x4) return sh.y32 ? launch_typed<true, float>(a, st) : launch_typed<true, __bf16>(a, st);
     return sh.y32 ? launch_typed<false, float>(a, st) : launch_typed<false, __bf16>(a, st);
 }

@@ -56,6 +56,8 @@ def test_first_stage(functions):
                 run.append(kind)
             elif kind == "end":
                 ahead, run = True, []
+            elif ahead and what == 0:
+                run = []                                                # everything has arrived
             elif ahead:
                 lds = [j for j, k in enumerate(run) if k == "lds"]
                 per = len(lds) // nb                                    # token loads of a stage: as many as blocks of 32 tokens, and a scale
