@@ -8,8 +8,9 @@
 // pass reads them once.  exp(v - m) is 2^((v - m) log2 e), the difference first: m log2 e on its own would overflow where all logits
 // are the type's lowest value.
 //
-// Bound by bytes for large batches and by the launch for small ones; the vector operations per logit (about 10 forward, 14
-// backward, and 5 for each further expert per token) take half as long as the bytes do.
+// Small batches are bound by the launch.  Large ones, forward, by the vector instructions, about 10 for a logit and 6 more for each
+// expert a token has (32768 tokens of 256 fp32 logits, 3 experts each: 14 us for 34 MB, and 4.6 us for the sums; 107351 of 239, 8
+// each: 56 us for 110 MB).  Backward, about 14 for a logit, by bytes: 262144 of 128 fp32 logits, 270 MB in 45 us, 6.0 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -81,24 +82,25 @@ struct Row {
     typedef __attribute__((ext_vector_type(VEC))) T Vec;
     float v[V];
     static __device__ __forceinline__ int column(int sub, int i) { return ((i / VEC) * kLanes + sub) * VEC + i % VEC; }
-    __device__ __forceinline__ void load(const T *row, int sub, int E)
-    {
+    // As they lie in memory, without a branch or a conversion that would wait for them (one load for each value, as where E is odd, would be
+    // waited for one by one: 40000 tokens of 129 bf16 logits, 14.7 us against 17.8); lanes past E read the first columns.
+    struct Raw {
+        Vec x[J];
+        __device__ __forceinline__ void load(const T *row, int sub, int E)
+        {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = (j * kLanes + sub) * VEC;
-            if (c < E) {                        // E is a multiple of VEC
-                if constexpr (VEC == 1) {
-                    v[j] = (float)row[c];
-                } else {
-                    const Vec x = *reinterpret_cast<const Vec *>(row + c);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) v[j * VEC + i] = (float)x[i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[j * VEC + i] = -INFINITY;
+            for (int j = 0; j < J; ++j) {
+                const int c = (j * kLanes + sub) * VEC;
+                x[j] = *reinterpret_cast<const Vec *>(row + (c < E ? c : 0));   // E is a multiple of VEC
             }
         }
+    };
+    __device__ __forceinline__ void take(const Raw &raw, int sub, int E)
+    {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[j * VEC + i] = (j * kLanes + sub) * VEC < E ? (float)raw.x[j][i] : -INFINITY;
     }
     __device__ __forceinline__ void store(T *row, int sub, int E) const
     {
@@ -184,14 +186,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_rows(const RouteArgs a)
 #pragma unroll
     for (int i = 0; i < R::V; ++i) p_acc[i] = 0;
     const int64_t step = (int64_t)gridDim.x * kRouteRows;
-    R next;
+    typename R::Raw next;
+    uint8_t next_in;
+    auto ask = [&](int64_t t) {
+        const T *row = (const T *)a.logits + t * a.ld;
+        next.load(row, sub, a.E);
+        next_in = *(a.mask ? a.mask + t : (const uint8_t *)row);   // no branch here either: a load behind one is waited for at once
+    };
     int64_t t = (int64_t)blockIdx.x * kRouteRows + tid / kLanes;
-    if (t < a.T) next.load((const T *)a.logits + t * a.ld, sub, a.E);
+    if (t < a.T) ask(t);
     for (; t < a.T; t += step) {
-        R r = next;
-        if (t + step < a.T) next.load((const T *)a.logits + (t + step) * a.ld, sub, a.E);   // while this token is dealt with
+        R r;
+        r.take(next, sub, a.E);
+        const bool in = !a.mask || next_in;
+        if (t + step < a.T) ask(t + step);                   // while this token is dealt with
         const float m = r.largest();
-        const bool part = (!a.mask || a.mask[t]) && !r.nothing(m);
+        const bool part = in && !r.nothing(m);
         float e[R::V], sum = 0;
 #pragma unroll
         for (int i = 0; i < R::V; ++i) {
@@ -366,13 +376,31 @@ template <class T, int VEC, int J>
 __global__ __launch_bounds__(kBackThreads) void route_back_rows(const RouteArgs a)
 {
     typedef Row<T, VEC, J> R;
-    const int tid = threadIdx.x, sub = tid & (kLanes - 1);
+    const int tid = threadIdx.x, sub = tid & (kLanes - 1), lane = tid & 63;
+    // What is read of a token: its logits, and in lane j its j-th expert and the gradient of its gate (36000 tokens of 128 bf16 logits, 8
+    // experts each, 12.9 us; every lane loading every one of them, one behind the other, 19.7).
+    typename R::Raw next;
+    uint8_t next_in;
+    int next_id = -1;
+    float next_dg = 0;
+    auto ask = [&](int64_t t) {
+        const T *row = (const T *)a.logits + t * a.ld;
+        next.load(row, sub, a.E);
+        next_in = *(a.mask ? a.mask + t : (const uint8_t *)row);
+        if (a.d_gates && sub < a.k) {
+            next_id = a.ids[t * a.k + sub];
+            next_dg = a.d_gates[t * a.k + sub];
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * kBackRows;
+    int64_t t = (int64_t)blockIdx.x * kBackRows + tid / kLanes;
+    if (t < a.T) ask(t);
     // What the loss adds to an expert's column: d_loss E/n counts/(n k), n k being the sum of all counts.
     float pull[R::V];
     int all = 0;
 #pragma unroll
     for (int i = 0; i < R::V; ++i) {
-        const int c = R::column(sub, i), n = c < a.E ? a.counts[c] : 0;
+        const int c = R::column(sub, i), at = a.counts[c < a.E ? c : 0], n = c < a.E ? at : 0;
         all += n;
         pull[i] = (float)n;
     }
@@ -380,12 +408,16 @@ __global__ __launch_bounds__(kBackThreads) void route_back_rows(const RouteArgs 
     const float nk = (float)all, coef = a.d_loss && all ? *a.d_loss * (float)a.E * (float)a.k / nk / nk : 0.f;
 #pragma unroll
     for (int i = 0; i < R::V; ++i) pull[i] *= coef;
-    for (int64_t t = (int64_t)blockIdx.x * kBackRows + tid / kLanes; t < a.T; t += (int64_t)gridDim.x * kBackRows) {
-        const T *row = (const T *)a.logits + t * a.ld;
+    for (; t < a.T; t += step) {
         R r;
-        r.load(row, sub, a.E);
+        r.take(next, sub, a.E);
+        const bool in = !a.mask || next_in;
+        const int my_id = (uint32_t)next_id < (uint32_t)a.E ? next_id : -1;   // a place past E is no expert's
+        const float my_dg = next_dg;
+        const T my_logit = ((const T *)a.logits + t * a.ld)[my_id >= 0 ? my_id : 0];
+        if (t + step < a.T) ask(t + step);                   // while this token is dealt with
         const float m = r.largest();
-        const bool part = (!a.mask || a.mask[t]) && !r.nothing(m);
+        const bool part = in && !r.nothing(m);
         float p[R::V], sum = 0;
 #pragma unroll
         for (int i = 0; i < R::V; ++i) {
@@ -400,24 +432,15 @@ __global__ __launch_bounds__(kBackThreads) void route_back_rows(const RouteArgs 
             d[i] = pull[i];
         }
         if (a.d_gates) {
-            const int32_t *ids = a.ids + t * a.k;
-            const float *dg = a.d_gates + t * a.k;
-            float mean = 0, scale = 1;
-            if (a.normalize) {                               // sum_i dg_i gate_i, and one over the sum of the chosen p
-                float chosen = 0;
-                for (int j = 0; j < a.k; ++j) {
-                    const int id = ids[j];
-                    if ((uint32_t)id >= (uint32_t)a.E) continue;
-                    const float q = power((float)row[id], m) * inv;
-                    chosen += q;
-                    mean += dg[j] * q;
-                }
-                scale = 1.f / chosen;
-                mean *= scale;
+            float my_g = my_dg;
+            if (a.normalize) {                               // dg_i - sum_j dg_j gate_j, over the sum of the chosen p
+                const float q = my_id >= 0 ? power((float)my_logit, m) * inv : 0.f;
+                const float scale = 1.f / row_sum(q);
+                my_g = (my_dg - row_sum(my_id >= 0 ? my_dg * q : 0.f) * scale) * scale;
             }
             for (int j = 0; j < a.k; ++j) {
-                const int id = (uint32_t)ids[j] < (uint32_t)a.E ? ids[j] : -1;   // a place past E is no expert's
-                const float g = (dg[j] - mean) * scale;
+                const int from = (lane & ~(kLanes - 1)) + j, id = __shfl(my_id, from);
+                const float g = __shfl(my_g, from);
 #pragma unroll
                 for (int i = 0; i < R::V; ++i) d[i] += R::column(sub, i) == id ? g : 0.f;
             }
