@@ -185,19 +185,23 @@ def hash_forward_static(cfg: SidaHashConfig, params, x, n_seq, seq_len, ids, alp
 
 # ---- experts in 4 bits and the router: torch tensors in, types and shapes from them.  What a C entry cannot see (a tensor's
 # type, its inner stride, its size) is checked here, the rest there.
-_KINDS = {}                              # torch.dtype -> SIDA_BF16 / SIDA_FP32, and the dtypes by name; filled at the first call
+# A small call's time is the host's: each attribute of a tensor is asked for once.
+class _Kinds(dict):
+    """torch.dtype -> SIDA_BF16 / SIDA_FP32 (None: neither), and the dtypes by name; filled when first asked."""
+
+    def __missing__(self, key):
+        if not self:
+            import torch
+            self.update({torch.bfloat16: BF16, torch.float32: FP32, "bf16": (torch.bfloat16,), "fp32": (torch.float32,),
+                         "uint8": (torch.uint8,), "int32": (torch.int32,), "bool": (torch.bool, torch.uint8)})
+        return self.get(key)
 
 
-def _kinds():
-    if not _KINDS:
-        import torch
-        _KINDS.update({torch.bfloat16: BF16, torch.float32: FP32, "bf16": (torch.bfloat16,), "fp32": (torch.float32,), "uint8": (torch.uint8,),
-                       "int32": (torch.int32,), "bool": (torch.bool, torch.uint8)})
-    return _KINDS
+_KINDS = _Kinds()
 
 
 def _type(t) -> int:
-    kind = _kinds().get(t.dtype)
+    kind = _KINDS[t.dtype]
     if kind is None:
         raise ValueError(f"bf16 or fp32 values are needed, not {t.dtype}")
     return kind
@@ -205,9 +209,10 @@ def _type(t) -> int:
 
 def _rows(t, what: str):
     """(rows, columns, values between rows) of a matrix on the GPU whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{what}: a matrix on the GPU is needed")
-    rows, cols = t.shape
+    rows, cols = shape
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
         raise ValueError(f"{what}: contiguous rows are needed")
@@ -216,7 +221,7 @@ def _rows(t, what: str):
 
 def _flat(t, n: int, kind: str, what: str):
     """Address of t, which holds at least n values of a type, one after the other, on the GPU."""
-    if t.dtype not in _kinds()[kind] or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype not in _KINDS[kind] or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{what}: a contiguous tensor of at least {n} {kind} values on the GPU is needed")
     return t.data_ptr()
 
@@ -250,9 +255,9 @@ def mx_quantize(x, codes, scales, stream, layout=MX_ROWS, values=None):
     """x: bf16 or fp32 [rows, cols]; codes, scales: uint8, mx_codes_bytes and mx_scales_bytes of them; values: bf16 [rows, cols] or None."""
     rows, cols, ld = _rows(x, "x")
     n_codes, n_scales = _mx_bytes(rows, cols, layout)
-    rc = lib().sida_mx_quantize(x.data_ptr(), _type(x), rows, cols, ld, layout, _flat(codes, n_codes, "uint8", "codes"),
-                                _flat(scales, n_scales, "uint8", "scales"),
-                                None if values is None else _flat(values, rows * cols, "bf16", "values"), _stream(stream))
+    rc = (_LIB or lib()).sida_mx_quantize(
+        x.data_ptr(), _type(x), rows, cols, ld, layout, _flat(codes, n_codes, "uint8", "codes"), _flat(scales, n_scales, "uint8", "scales"),
+        None if values is None else _flat(values, rows * cols, "bf16", "values"), _stream(stream))
     if rc:
         raise SidaError(rc, "sida_mx_quantize")
 
@@ -268,15 +273,16 @@ def mx_gemm(x, x_scales, codes, scales, offsets, y, stream, relu=False):
             raise ValueError("x: codes have to be contiguous")
         K, ldx, kind = 2 * K, 2 * ldx, MXFP4
         xs = _flat(x_scales, _mx_bytes(M, K, MX_ROWS)[1], "uint8", "x_scales")
-    if x.dtype not in _kinds()["bf16" if xs is None else "uint8"]:
+    if x.dtype not in _KINDS["bf16" if xs is None else "uint8"]:
         raise ValueError(f"x: bf16 values, or uint8 codes with their scales, are needed, not {x.dtype}")
     if rows != M:
         raise ValueError(f"y: {M} rows are needed, not {rows}")
     groups = 1 if offsets is None else offsets.numel() - 1
     n_codes, n_scales = _mx_bytes(N, K, MX_TILES)
-    rc = lib().sida_mx_gemm(_gemm_config(groups, N, K, kind, _type(y), 1 if relu else 0)[1], x.data_ptr(), xs, ldx, M,
-                            _flat(codes, groups * n_codes, "uint8", "codes"), _flat(scales, groups * n_scales, "uint8", "scales"),
-                            None if offsets is None else _flat(offsets, 1, "int32", "offsets"), y.data_ptr(), ldy, _stream(stream))
+    rc = (_LIB or lib()).sida_mx_gemm(
+        _gemm_config(groups, N, K, kind, _type(y), 1 if relu else 0)[1], x.data_ptr(), xs, ldx, M,
+        _flat(codes, groups * n_codes, "uint8", "codes"), _flat(scales, groups * n_scales, "uint8", "scales"),
+        None if offsets is None else _flat(offsets, 1, "int32", "offsets"), y.data_ptr(), ldy, _stream(stream))
     if rc:
         raise SidaError(rc, "sida_mx_gemm")
 
@@ -287,31 +293,35 @@ def route_workspace_bytes(cfg: SidaRouteConfig, T: int) -> int:
 
 def _route_args(logits, ids, counts, mask, normalize):
     T, E, ld = _rows(logits, "logits")
-    if ids.dim() != 2 or ids.shape[0] != T:
+    shape = ids.shape
+    if len(shape) != 2 or shape[0] != T:
         raise ValueError(f"ids: [{T}, experts per token] are needed")
-    k = ids.shape[1]
-    return (_route_config(E, k, _type(logits), 1 if normalize else 0)[1], T, k, ld, None if mask is None else _flat(mask, T, "bool", "mask"),
+    k = shape[1]
+    kind = _type(logits)
+    return (_route_config(E, k, kind, 1 if normalize else 0)[1], T, E, k, kind, ld, None if mask is None else _flat(mask, T, "bool", "mask"),
             _flat(ids, T * k, "int32", "ids"), _flat(counts, E, "int32", "counts"))
 
 
 def route(logits, ids, gates, counts, loss, workspace, stream, mask=None, normalize=False):
     """logits: bf16 or fp32 [T, E]; ids: int32 [T, k]; gates: fp32 [T, k]; counts: int32 [E]; loss: fp32, one value; workspace: uint8,
     route_workspace_bytes of it; mask: bool or uint8 [T] or None."""
-    cfg, T, k, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
-    rc = lib().sida_route(cfg, logits.data_ptr(), ld, T, m, i, _flat(gates, T * k, "fp32", "gates"), c, _flat(loss, 1, "fp32", "loss"),
-                          _flat(workspace, 0, "uint8", "workspace"), workspace.numel(), _stream(stream))
+    cfg, T, _, k, _, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
+    rc = (_LIB or lib()).sida_route(
+        cfg, logits.data_ptr(), ld, T, m, i, _flat(gates, T * k, "fp32", "gates"), c, _flat(loss, 1, "fp32", "loss"),
+        _flat(workspace, 0, "uint8", "workspace"), workspace.numel(), _stream(stream))
     if rc:
         raise SidaError(rc, "sida_route")
 
 
 def route_backward(logits, ids, counts, d_logits, stream, d_gates=None, d_loss=None, mask=None, normalize=False):
     """d_logits: as logits; d_gates: fp32 [T, k] or None; d_loss: fp32, one value, or None."""
-    cfg, T, k, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
-    if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
+    cfg, T, E, k, kind, ld, m, i, c = _route_args(logits, ids, counts, mask, normalize)
+    rows, cols, ld_d = _rows(d_logits, "d_logits")
+    if rows != T or cols != E or _KINDS[d_logits.dtype] != kind:
         raise ValueError("d_logits: shape and type of the logits are needed")
-    rc = lib().sida_route_backward(cfg, logits.data_ptr(), ld, T, m, i, c, None if d_gates is None else _flat(d_gates, T * k, "fp32", "d_gates"),
-                                   None if d_loss is None else _flat(d_loss, 1, "fp32", "d_loss"), d_logits.data_ptr(),
-                                   _rows(d_logits, "d_logits")[2], _stream(stream))
+    rc = (_LIB or lib()).sida_route_backward(
+        cfg, logits.data_ptr(), ld, T, m, i, c, None if d_gates is None else _flat(d_gates, T * k, "fp32", "d_gates"),
+        None if d_loss is None else _flat(d_loss, 1, "fp32", "d_loss"), d_logits.data_ptr(), ld_d, _stream(stream))
     if rc:
         raise SidaError(rc, "sida_route_backward")
 
