@@ -2,6 +2,8 @@
 combine, and the gradient that trains the router.  Buffers and streams only; the arithmetic is the library's."""
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from .binding import (BF16, FP32, MX_TILES, Context, SidaRouteConfig, mx_codes_bytes, mx_gemm, mx_quantize, mx_scales_bytes,
@@ -12,14 +14,24 @@ class MxMoELayer:
     """y[t,:] = sum_j gates[t,j] * W_out[e] relu(W_in[e] x[t,:]), e = ids[t,j] the top_k experts of logits[t,:].
 
     The weights take 17/64 of their bf16 bytes.  tokens_in_4_bits: x and the hidden values are rounded to MXFP4 too, and
-    multiplied in 4 bits.  Everything is enqueued on `stream` (default: torch's current one when the layer is made); results are views of the
-    layer's buffers and hold until its next forward call."""
+    multiplied in 4 bits.  Everything is enqueued on `stream` (a torch stream or a raw one; default: torch's current one when the layer is
+    made).  It goes on behind what torch's current stream has been given when a call is made, and the current stream goes on behind the call, so that
+    inputs, results and the memory of both are used as on the current stream alone.  y and the gradient are new tensors; the loss, ids, gates
+    and counts are views of the layer's buffers and hold until its next forward call."""
 
     def __init__(self, E, d_model, d_ff, max_tokens, top_k=1, normalize=False, tokens_in_4_bits=False, device="cuda:0", stream=None):
         self.dev = torch.device(device)
         self.E, self.d, self.F, self.k, self.normalize, self.x4 = E, d_model, d_ff, top_k, normalize, tokens_in_4_bits
         self.max_pairs = max_tokens * top_k
-        self.stream = stream if stream is not None else torch.cuda.current_stream(self.dev)
+        if stream is None:
+            stream = torch.cuda.current_stream(self.dev)
+        elif isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.dev) if stream else torch.cuda.default_stream(self.dev)
+        self.stream = stream
+        with self._on_stream():                                            # the buffers' memory is that stream's
+            self._make_buffers(E, d_model, d_ff, max_tokens, top_k)
+
+    def _make_buffers(self, E, d_model, d_ff, max_tokens, top_k):
         self.ctx = Context(1, E, d_model, d_ff, 1, 1, self.max_pairs)      # sort and combine; its expert pool stays unbound
         self.ctx.set_top_k(top_k)
         self.workspace = self._buffer(max(256, self.ctx.workspace_bytes(self.max_pairs)))
@@ -31,18 +43,35 @@ class MxMoELayer:
         self.gates = torch.empty((max_tokens, top_k), device=self.dev)
         self.counts = torch.empty(E, dtype=torch.int32, device=self.dev)
         self.loss = torch.empty(1, device=self.dev)
-        if tokens_in_4_bits:
+        if self.x4:
             widest = max(d_model, d_ff)
             self.x_codes = self._buffer(self.max_pairs * widest // 2)
             self.x_scales = self._buffer(self.max_pairs * (-(-widest // 256) * 8))
+
+    @contextlib.contextmanager
+    def _on_stream(self, shown=()):
+        """The layer's stream is torch's current one inside.  shown: tensors of its memory that the caller goes on to use."""
+        caller = torch.cuda.current_stream(self.dev)
+        if caller == self.stream:
+            yield
+            return
+        self.stream.wait_stream(caller)
+        try:
+            with torch.cuda.stream(self.stream):
+                yield
+        finally:
+            caller.wait_stream(self.stream)
+            for t in shown:
+                t.record_stream(caller)
 
     def _buffer(self, nbytes):
         return torch.empty(nbytes, dtype=torch.uint8, device=self.dev)
 
     def load_experts(self, w_in, w_out):
         """w_in: bf16 or fp32 [E, d_ff, d_model], w_out [E, d_model, d_ff], on the GPU: rounded to MXFP4 and laid out."""
-        for w, (codes, scales) in zip((w_in, w_out), self.experts):
-            mx_quantize(w.reshape(-1, w.shape[2]), codes, scales, self.stream, layout=MX_TILES)   # rows are multiples of 128
+        with self._on_stream():
+            for w, (codes, scales) in zip((w_in, w_out), self.experts):
+                mx_quantize(w.reshape(-1, w.shape[2]), codes, scales, self.stream, layout=MX_TILES)   # rows are multiples of 128
 
     def _region(self, layout, name, dtype, shape):
         n = torch.empty((), dtype=dtype).element_size()
@@ -64,12 +93,17 @@ class MxMoELayer:
     def forward(self, x, logits, mask=None):
         """x: bf16 [T, d_model]; logits: bf16 or fp32 [T, E]; mask: bool [T] or None (a masked token's y is 0).  Returns y [T, d_model] and
         the balance loss [1]; ids, gates and counts are the layer's."""
+        y = torch.empty_like(x)                                            # memory of the caller's stream
+        with self._on_stream((self.ids, self.gates, self.counts, self.loss)):
+            self._forward(x, logits, mask, y)
+        return y, self.loss
+
+    def _forward(self, x, logits, mask, y):
         T, pairs = x.shape[0], x.shape[0] * self.k
-        y = torch.empty_like(x)
         ids, gates = self.ids[:T], self.gates[:T]
         route(logits, ids, gates, self.counts, self.loss, self.route_ws, self.stream, mask=mask, normalize=self.normalize)
         if T == 0:
-            return y, self.loss
+            return
         self.ctx.dispatch(x, ids, pairs, self.workspace, self.stream)
         lay = self.ctx.workspace_layout(pairs)
         offsets = self._region(lay, "offsets", torch.int32, (self.E + 1,))
@@ -79,7 +113,6 @@ class MxMoELayer:
         self._product(self._region(lay, "x_perm", torch.bfloat16, (pairs, self.d)), self.experts[0], offsets, h, True)
         self._product(h, self.experts[1], offsets, self.y_perm, False)
         self.ctx.combine(gates, pairs, y, self.workspace, self.stream)
-        return y, self.loss
 
     def router_gradient(self, logits, dy, d_loss, mask=None):
         """Gradient of the last forward call's logits from that of y (bf16 [T, d_model]) and of the balance loss (fp32 [1]).  A gate's is
@@ -87,10 +120,11 @@ class MxMoELayer:
         T = logits.shape[0]
         out = torch.empty_like(logits)
         if T:
-            rows = self.y_perm[self.inv.long()].view(T, self.k, self.d)
-            d_gates = (rows.float() * dy.float()[:, None, :]).sum(2)
-            route_backward(logits, self.ids[:T], self.counts, out, self.stream, d_gates=d_gates, d_loss=d_loss, mask=mask,
-                           normalize=self.normalize)
+            with self._on_stream():
+                rows = self.y_perm[self.inv.long()].view(T, self.k, self.d)
+                d_gates = (rows.float() * dy.float()[:, None, :]).sum(2)
+                route_backward(logits, self.ids[:T], self.counts, out, self.stream, d_gates=d_gates, d_loss=d_loss, mask=mask,
+                               normalize=self.normalize)
         return out
 
     def close(self):
