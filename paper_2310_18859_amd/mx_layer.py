@@ -21,8 +21,11 @@ class MxMoELayer:
 
     def __init__(self, E, d_model, d_ff, max_tokens, top_k=1, normalize=False, tokens_in_4_bits=False, device="cuda:0", stream=None):
         self.dev = torch.device(device)
+        if self.dev.type == "cuda" and self.dev.index is None:
+            self.dev = torch.device("cuda", torch.cuda.current_device())
+        self.loaded, self.tokens = False, 0                                # experts are there; tokens of the last forward call
         self.E, self.d, self.F, self.k, self.normalize, self.x4 = E, d_model, d_ff, top_k, normalize, tokens_in_4_bits
-        self.max_pairs = max_tokens * top_k
+        self.max_tokens, self.max_pairs = max_tokens, max_tokens * top_k
         if stream is None:
             stream = torch.cuda.current_stream(self.dev)
         elif isinstance(stream, int):
@@ -67,11 +70,21 @@ class MxMoELayer:
     def _buffer(self, nbytes):
         return torch.empty(nbytes, dtype=torch.uint8, device=self.dev)
 
+    # dispatch, combine and torch's operations take what they are given for the layer's own sizes: what a tensor has to be is checked here,
+    # before anything is enqueued.  The rest is checked by the calls that take it.
+    def _need(self, t, what, shape, dtypes=(torch.bfloat16, torch.float32)):
+        if tuple(t.shape) != shape or t.dtype not in dtypes or t.device != self.dev:
+            raise ValueError(f"{what}: {list(shape)} of {' or '.join(str(d) for d in dtypes)} on {self.dev} is needed, "
+                             f"not {list(t.shape)} of {t.dtype} on {t.device}")
+
     def load_experts(self, w_in, w_out):
         """w_in: bf16 or fp32 [E, d_ff, d_model], w_out [E, d_model, d_ff], on the GPU: rounded to MXFP4 and laid out."""
+        for w, what, shape in ((w_in, "w_in", (self.E, self.F, self.d)), (w_out, "w_out", (self.E, self.d, self.F))):
+            self._need(w, what, shape)
         with self._on_stream():
             for w, (codes, scales) in zip((w_in, w_out), self.experts):
                 mx_quantize(w.reshape(-1, w.shape[2]), codes, scales, self.stream, layout=MX_TILES)   # rows are multiples of 128
+        self.loaded = True
 
     def _region(self, layout, name, dtype, shape):
         n = torch.empty((), dtype=dtype).element_size()
@@ -91,11 +104,20 @@ class MxMoELayer:
         mx_gemm(x, scales, *weights, offsets, y, self.stream, relu=relu)
 
     def forward(self, x, logits, mask=None):
-        """x: bf16 [T, d_model]; logits: bf16 or fp32 [T, E]; mask: bool [T] or None (a masked token's y is 0).  Returns y [T, d_model] and
-        the balance loss [1]; ids, gates and counts are the layer's."""
-        y = torch.empty_like(x)                                            # memory of the caller's stream
+        """x: bf16 [T, d_model] (copied where it is not contiguous from a 16-byte boundary on); logits: bf16 or fp32 [T, E]; mask: bool [T] or
+        None (a masked token's y is 0).  Returns y [T, d_model] and the balance loss [1]; ids, gates and counts are the layer's."""
+        T = x.shape[0] if x.dim() else 0
+        self._need(x, "x", (T, self.d), (torch.bfloat16,))
+        if T > self.max_tokens:
+            raise ValueError(f"x: at most {self.max_tokens} tokens, not {T}")
+        self._need(logits, "logits", (T, self.E))
+        if T and not self.loaded:
+            raise RuntimeError("load_experts has not been called")
+        y = torch.empty((T, self.d), dtype=torch.bfloat16, device=self.dev)   # memory of the caller's stream
         with self._on_stream((self.ids, self.gates, self.counts, self.loss)):
-            self._forward(x, logits, mask, y)
+            x = x.contiguous()
+            self._forward(x.clone() if x.data_ptr() % 16 else x, logits, mask, y)
+        self.tokens = T
         return y, self.loss
 
     def _forward(self, x, logits, mask, y):
@@ -115,9 +137,11 @@ class MxMoELayer:
         self.ctx.combine(gates, pairs, y, self.workspace, self.stream)
 
     def router_gradient(self, logits, dy, d_loss, mask=None):
-        """Gradient of the last forward call's logits from that of y (bf16 [T, d_model]) and of the balance loss (fp32 [1]).  A gate's is
-        the product of dy with its expert's output."""
-        T = logits.shape[0]
+        """Gradient of the last forward call's logits (the same logits and mask are given again) from that of y (bf16 [T, d_model]) and of
+        the balance loss (fp32 [1]).  A gate's is the product of dy with its expert's output."""
+        T = self.tokens
+        self._need(logits, "logits", (T, self.E))
+        self._need(dy, "dy", (T, self.d), (torch.bfloat16, torch.float32, torch.float16, torch.float64))
         out = torch.empty_like(logits)
         if T:
             with self._on_stream():

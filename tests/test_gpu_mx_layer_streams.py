@@ -112,3 +112,18 @@ def test_other_streams(want, way, x4):
         del layer
         torch.cuda.empty_cache()
         streams_destroy(*raw)
+
+
+def test_strided_and_shifted_tokens(want):
+    """Rows with something between them, columns in another order and rows off a 16-byte boundary give what packed rows give."""
+    v, expected = want
+    layer = MxMoELayer(E, D, F, T, top_k=K, normalize=True)
+    layer.load_experts(v["w_in"], v["w_out"])
+    wide = torch.full((T, D + 8), float("nan"), dtype=torch.bfloat16, device=DEV)
+    wide[:, 8:] = v["x"]
+    shifted = torch.full((T * D + 1,), float("nan"), dtype=torch.bfloat16, device=DEV)[1:].view(T, D)
+    shifted.copy_(v["x"])
+    for x in (wide[:, 8:], v["x"].t().contiguous().t(), shifted):
+        y, _ = layer.forward(x, v["logits"], v["mask"])
+        assert y.is_contiguous() and torch.equal(y, expected[0])
+    layer.close()
