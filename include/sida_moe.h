@@ -336,6 +336,10 @@ int sida_grouped_ffn(sida_ctx *ctx, const sida_plan *plan, int32_t wave, void *w
 /* Gate-weighted scatter-combine only: y[t,:] = alpha[t] * y_perm[inv[t],:]. */
 int sida_combine(sida_ctx *ctx, const float *alpha_dev, int32_t T, void *y_dev,
                  void *workspace_dev, size_t workspace_bytes, void *stream);
+/* The same behind sida_route: a token that took no part (all of its top_k gates are 0) gets a row of zeros, also where its own
+ * values, and with them its experts' outputs, are infinite or NaN. */
+int sida_combine_routed(sida_ctx *ctx, const float *gates_dev, int32_t T, void *y_dev,
+                        void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* ---- the hash function of the hash-building thread (Section 3.4.2) ----------------------------
  * Predicts the hash table of a batch from the token embeddings alone: for every token and MoE

@@ -114,6 +114,7 @@ def lib():
         "sida_dispatch": (C.c_int, [vp, vp, vp, i32, vp, sz, vp]),
         "sida_grouped_ffn": (C.c_int, [vp, C.POINTER(SidaPlan), i32, vp, sz, vp]),
         "sida_combine": (C.c_int, [vp, vp, i32, vp, vp, sz, vp]),
+        "sida_combine_routed": (C.c_int, [vp, vp, i32, vp, vp, sz, vp]),
         "sida_profile_enable": (C.c_int, [vp, i32]),
         "sida_profile_read": (C.c_int, [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64), i32]),
         "sida_mx_codes_bytes": (sz, [C.c_int64, i32, i32]),
@@ -496,6 +497,10 @@ class Context:
     def combine(self, alpha, T, y, workspace, stream):
         self._ck(lib().sida_combine(self._h, _ptr(alpha), T, _ptr(y), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _stream(stream)), "sida_combine")
+
+    def combine_routed(self, gates, T, y, workspace, stream):
+        self._ck(lib().sida_combine_routed(self._h, _ptr(gates), T, _ptr(y), _ptr(workspace),
+                                           workspace.numel() * workspace.element_size(), _stream(stream)), "sida_combine_routed")
 
     # ---- timing
     def profile_enable(self, on: bool):

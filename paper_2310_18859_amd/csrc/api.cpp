@@ -970,8 +970,9 @@ int sida_grouped_ffn(sida_ctx *c, const sida_plan *plan, int32_t wave, void *wor
     return launch_wave_ffn(c, sched, wave, ws, plan->T, static_cast<hipStream_t>(stream));
 }
 
-int sida_combine(sida_ctx *c, const float *alpha_dev, int32_t T, void *y_dev, void *workspace_dev,
-                 size_t workspace_bytes, void *stream)
+namespace {
+int combine(sida_ctx *c, const float *alpha_dev, int32_t T, void *y_dev, void *workspace_dev, size_t workspace_bytes, void *stream,
+            bool routed)
 {
     if (!c || T < 0 || T > c->cfg.max_T || T % c->top_k) return SIDA_EINVAL;
     if (T == 0) return SIDA_OK;
@@ -981,8 +982,21 @@ int sida_combine(sida_ctx *c, const float *alpha_dev, int32_t T, void *y_dev, vo
     const Ws ws = carve(c->cfg, T, workspace_dev);
     hipStream_t st = static_cast<hipStream_t>(stream);
     TimedKernel tk(c, SIDA_K_COMBINE);
-    HIP_TRY(c, (hipError_t)launch_combine(ws.y_perm, ws.inv, alpha_dev, T, c->cfg.d_model, y_dev, st, tk.get(), c->top_k));
+    HIP_TRY(c, (hipError_t)launch_combine(ws.y_perm, ws.inv, alpha_dev, T, c->cfg.d_model, y_dev, st, tk.get(), c->top_k, routed));
     return SIDA_OK;
+}
+}  // namespace
+
+int sida_combine(sida_ctx *c, const float *alpha_dev, int32_t T, void *y_dev, void *workspace_dev,
+                 size_t workspace_bytes, void *stream)
+{
+    return combine(c, alpha_dev, T, y_dev, workspace_dev, workspace_bytes, stream, false);
+}
+
+int sida_combine_routed(sida_ctx *c, const float *gates_dev, int32_t T, void *y_dev, void *workspace_dev,
+                        size_t workspace_bytes, void *stream)
+{
+    return combine(c, gates_dev, T, y_dev, workspace_dev, workspace_bytes, stream, true);
 }
 
 // ---- hash function ---------------------------------------------------------------------------

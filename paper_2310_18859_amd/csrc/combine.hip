@@ -2,6 +2,8 @@
 // the expert outputs go back from expert order to token order:
 //     y[t,:] = sum_{j<k} alpha[t*k+j] * y_perm[inv[t*k+j],:]        (k = 1 for Switch routing)
 // Products and sum in fp32, terms in the order j = 0..k-1, one rounding to bf16 (nearest even).
+// Behind a router (ROUTED) a token takes no part where all of its factors are 0: its row is 0, whatever the expert rows hold (0 times an
+// infinity or NaN is NaN), and they are not read.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -17,6 +19,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 // source rows and gate values go to LDS first, then the rows' pieces are dealt to the 256 threads
 // as one flat range, so that no lane idles whatever the row length (96 pieces at d = 768).
 constexpr int kCombineRows = 8;
+template <bool ROUTED>
 __global__ __launch_bounds__(256) void combine_rows(const bf16x8 *__restrict__ y_perm,
                                                     const int32_t *__restrict__ inv,
                                                     const float *__restrict__ alpha, int n_tokens,
@@ -35,6 +38,14 @@ __global__ __launch_bounds__(256) void combine_rows(const bf16x8 *__restrict__ y
     bf16x8 *dst = y + (size_t)t0 * vec_per_row;               // its token rows are one contiguous range
     for (int p = threadIdx.x; p < n; p += 256) {
         const int r = p / vec_per_row, i = p - r * vec_per_row;
+        if constexpr (ROUTED) {
+            bool part = false;
+            for (int s = 0; s < k; ++s) part |= gate[r * k + s] != 0.f;   // also where it is NaN
+            if (!part) {
+                dst[p] = bf16x8{};
+                continue;
+            }
+        }
         float acc[8];
         {
             const float a = gate[r * k];
@@ -58,10 +69,10 @@ __global__ __launch_bounds__(256) void combine_rows(const bf16x8 *__restrict__ y
 }  // namespace
 
 int launch_combine(const void *y_perm, const int32_t *inv, const float *alpha, int32_t T, int32_t d,
-                   void *y, hipStream_t st, const LaunchEvents *ev, int32_t k)
+                   void *y, hipStream_t st, const LaunchEvents *ev, int32_t k, bool routed)
 {
     const int n_tokens = T / k;
-    hipExtLaunchKernelGGL(combine_rows, dim3((n_tokens + kCombineRows - 1) / kCombineRows), dim3(256), 0, st, ev ? ev->start : nullptr,
+    hipExtLaunchKernelGGL(routed ? combine_rows<true> : combine_rows<false>, dim3((n_tokens + kCombineRows - 1) / kCombineRows), dim3(256), 0, st, ev ? ev->start : nullptr,
                           ev ? ev->stop : nullptr, 0, (const bf16x8 *)y_perm, inv, alpha, n_tokens, d / 8,
                           (bf16x8 *)y, k);
     return (int)hipGetLastError();

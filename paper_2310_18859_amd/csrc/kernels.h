@@ -97,9 +97,10 @@ void forget_stream(hipStream_t st);
 // entries in table order; counts come from `offsets` (device).  At most max_tiles are written.
 int launch_build_tiles(const LayerTable &tbl, const int32_t *offsets, TileDesc *tiles, int32_t max_tiles,
                        hipStream_t st);
-// K-c: y[t,:] = sum_{j<k} alpha[t*k+j] * y_perm[inv[t*k+j],:]; T = rows of y_perm (k per token).
+// K-c: y[t,:] = sum_{j<k} alpha[t*k+j] * y_perm[inv[t*k+j],:]; T = rows of y_perm (k per token); routed: a token whose
+// alphas are all 0 gets zeros.
 int launch_combine(const void *y_perm, const int32_t *inv, const float *alpha, int32_t T, int32_t d,
-                   void *y, hipStream_t st, const LaunchEvents *ev = nullptr, int32_t k = 1);
+                   void *y, hipStream_t st, const LaunchEvents *ev = nullptr, int32_t k = 1, bool routed = false);
 
 // Prefetch by kernel: up to kCopyBatch experts per launch, src = pinned host block (device-visible
 // address), dst = pool slot.  expert_bytes is a multiple of 16.

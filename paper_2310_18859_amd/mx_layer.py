@@ -105,7 +105,7 @@ class MxMoELayer:
 
     def forward(self, x, logits, mask=None):
         """x: bf16 [T, d_model] (copied where it is not contiguous from a 16-byte boundary on); logits: bf16 or fp32 [T, E]; mask: bool [T] or
-        None (a masked token's y is 0).  Returns y [T, d_model] and the balance loss [1]; ids, gates and counts are the layer's."""
+        None (y is 0 where a token is masked, or all its logits are -infinity, whatever its x holds).  Returns y [T, d_model] and the balance loss [1]; ids, gates and counts are the layer's."""
         T = x.shape[0] if x.dim() else 0
         self._need(x, "x", (T, self.d), (torch.bfloat16,))
         if T > self.max_tokens:
@@ -134,7 +134,7 @@ class MxMoELayer:
         self.inv = self._region(lay, "inv", torch.int32, (pairs,))
         self._product(self._region(lay, "x_perm", torch.bfloat16, (pairs, self.d)), self.experts[0], offsets, h, True)
         self._product(h, self.experts[1], offsets, self.y_perm, False)
-        self.ctx.combine(gates, pairs, y, self.workspace, self.stream)
+        self.ctx.combine_routed(gates, pairs, y, self.workspace, self.stream)
 
     def router_gradient(self, logits, dy, d_loss, mask=None):
         """Gradient of the last forward call's logits (the same logits and mask are given again) from that of y (bf16 [T, d_model]) and of
