@@ -16,7 +16,7 @@ class MxMoELayer:
     The weights take 17/64 of their bf16 bytes.  tokens_in_4_bits: x and the hidden values are rounded to MXFP4 too, and
     multiplied in 4 bits.  Everything is enqueued on `stream` (a torch stream or a raw one; default: torch's current one when the layer is
     made).  It goes on behind what torch's current stream has been given when a call is made, and the current stream goes on behind the call, so that
-    inputs, results and the memory of both are used as on the current stream alone.  y and the gradient are new tensors; the loss, ids, gates
+    inputs, results and the memory of both are used as on the current stream alone.  `device` need not be the current one.  y and the gradient are new tensors; the loss, ids, gates
     and counts are views of the layer's buffers and hold until its next forward call."""
 
     def __init__(self, E, d_model, d_ff, max_tokens, top_k=1, normalize=False, tokens_in_4_bits=False, device="cuda:0", stream=None):
@@ -53,19 +53,21 @@ class MxMoELayer:
 
     @contextlib.contextmanager
     def _on_stream(self, shown=()):
-        """The layer's stream is torch's current one inside.  shown: tensors of its memory that the caller goes on to use."""
-        caller = torch.cuda.current_stream(self.dev)
-        if caller == self.stream:
-            yield
-            return
-        self.stream.wait_stream(caller)
-        try:
-            with torch.cuda.stream(self.stream):
+        """The layer's stream is torch's current one inside, and its device the current one: the library's calls go to that, and the default
+        streams of all devices have the same raw value.  shown: tensors of the stream's memory that the caller goes on to use."""
+        with torch.cuda.device(self.dev):
+            caller = torch.cuda.current_stream(self.dev)
+            if caller == self.stream:
                 yield
-        finally:
-            caller.wait_stream(self.stream)
-            for t in shown:
-                t.record_stream(caller)
+                return
+            self.stream.wait_stream(caller)
+            try:
+                with torch.cuda.stream(self.stream):
+                    yield
+            finally:
+                caller.wait_stream(self.stream)
+                for t in shown:
+                    t.record_stream(caller)
 
     def _buffer(self, nbytes):
         return torch.empty(nbytes, dtype=torch.uint8, device=self.dev)
