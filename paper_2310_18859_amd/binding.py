@@ -227,27 +227,40 @@ def _flat(t, n: int, kind: str, what: str):
     return t.data_ptr()
 
 
+# A C argument of 32 bits takes a larger Python integer's lower ones without a word.
+def _is_int32(*sizes) -> bool:
+    return all(-1 << 31 <= n < 1 << 31 for n in sizes)
+
+
+def _need_int32(*sizes):
+    if not _is_int32(*sizes):
+        raise ValueError(f"sizes below 2^31 are needed, not {max(sizes, key=abs)}")
+
+
 def mx_codes_bytes(rows: int, cols: int, layout: int) -> int:
-    return lib().sida_mx_codes_bytes(rows, cols, layout)
+    return lib().sida_mx_codes_bytes(rows, cols, layout) if _is_int32(rows >> 32, cols, layout) else 0
 
 
 def mx_scales_bytes(rows: int, cols: int, layout: int) -> int:
-    return lib().sida_mx_scales_bytes(rows, cols, layout)
+    return lib().sida_mx_scales_bytes(rows, cols, layout) if _is_int32(rows >> 32, cols, layout) else 0
 
 
 @functools.lru_cache(maxsize=1024)
 def _mx_bytes(rows: int, cols: int, layout: int):
-    return lib().sida_mx_codes_bytes(rows, cols, layout), lib().sida_mx_scales_bytes(rows, cols, layout)
+    _need_int32(cols, layout)
+    return mx_codes_bytes(rows, cols, layout), mx_scales_bytes(rows, cols, layout)
 
 
 @functools.lru_cache(maxsize=1024)
 def _gemm_config(*fields):
+    _need_int32(*fields)
     cfg = SidaMxGemmConfig(*fields)
     return cfg, C.byref(cfg)
 
 
 @functools.lru_cache(maxsize=1024)
 def _route_config(*fields):
+    _need_int32(*fields)
     cfg = SidaRouteConfig(*fields)
     return cfg, C.byref(cfg)
 
@@ -278,6 +291,8 @@ def mx_gemm(x, x_scales, codes, scales, offsets, y, stream, relu=False):
         raise ValueError(f"x: bf16 values, or uint8 codes with their scales, are needed, not {x.dtype}")
     if rows != M:
         raise ValueError(f"y: {M} rows are needed, not {rows}")
+    if M >= 1 << 31:
+        _need_int32(M)
     groups = 1 if offsets is None else offsets.numel() - 1
     n_codes, n_scales = _mx_bytes(N, K, MX_TILES)
     rc = (_LIB or lib()).sida_mx_gemm(
@@ -289,7 +304,7 @@ def mx_gemm(x, x_scales, codes, scales, offsets, y, stream, relu=False):
 
 
 def route_workspace_bytes(cfg: SidaRouteConfig, T: int) -> int:
-    return lib().sida_route_workspace_bytes(C.byref(cfg), T)
+    return lib().sida_route_workspace_bytes(C.byref(cfg), T) if _is_int32(T) else 0
 
 
 def _route_args(logits, ids, counts, mask, normalize):
@@ -297,6 +312,8 @@ def _route_args(logits, ids, counts, mask, normalize):
     shape = ids.shape
     if len(shape) != 2 or shape[0] != T:
         raise ValueError(f"ids: [{T}, experts per token] are needed")
+    if T >= 1 << 31:
+        _need_int32(T)
     k = shape[1]
     kind = _type(logits)
     return (_route_config(E, k, kind, 1 if normalize else 0)[1], T, E, k, kind, ld, None if mask is None else _flat(mask, T, "bool", "mask"),
