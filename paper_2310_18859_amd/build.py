@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsida_moe.so")
 SOURCES = ["api.cpp", "plan.cpp", "sort_gather.hip", "grouped_ffn.hip", "combine.hip", "prefetch.hip", "hash_fn.hip", "debug.hip",
            "api_ops.cpp", "mx_quant.hip", "mx_gemm.hip", "route.hip"]
-HEADERS = ["ctx.h", "kernels.h", "tile_order.h", "handover.h", "past_end.h", "lds_grant.h", "tile_rule.h", "heads_walk.h"]
+HEADERS = ["ctx.h", "kernels.h", "tile_order.h", "handover.h", "past_end.h", "lds_grant.h", "tile_rule.h", "heads_walk.h", "mx_rule.h"]
 
 
 def _newest_source() -> float:

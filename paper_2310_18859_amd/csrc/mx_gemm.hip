@@ -21,6 +21,7 @@
 #include <utility>
 
 #include "kernels.h"
+#include "mx_rule.h"
 
 namespace sida {
 
@@ -469,25 +470,18 @@ int launch_shape(const MxArgs &a, hipStream_t st)
 template <bool X4, class Y>
 int launch_typed(const MxArgs &a, hipStream_t st)
 {
-    // The sum over K split over a workgroup, or 128 columns to a workgroup and K in one go.  The first takes 3.3 us for each round of 256
-    // stripes (1 token, 4096 x 1024: 6.2 us against 17.5; 16 tokens of 64 experts, 4096 x 1024, 512 stripes: 11.9 against 19.9), the second 4.5 us and
-    // 0.2 for each 64 of K in up to a thousand stripes (8 tokens of 8 experts, 768 x 3072, 768 stripes: 6.7 us against 10.4;
-    // 64 of 64, 3072 x 768, 1536 stripes: 20.6 against 27.0).
-    const int64_t few = (a.M / 32 + (a.groups < a.M ? a.groups : a.M)) * (int64_t)((a.N + 31) / 32);
-    if (few <= a.K / 4) {
-        mx_gemm_split<X4, Y><<<(uint32_t)((few + 7) / 8 * 8), kSplit * 64, 0, st>>>(a);
+    switch (mx_tiles(X4, a.M, a.groups, a.N, a.K)) {
+    case MxTiles::split: {
+        const int64_t tiles = (a.M / 32 + (a.groups < a.M ? a.groups : a.M)) * (int64_t)((a.N + 31) / 32);
+        mx_gemm_split<X4, Y><<<(uint32_t)((tiles + 7) / 8 * 8), kSplit * 64, 0, st>>>(a);
         return (int)hipGetLastError();
     }
-    // Tile height and width, by how many rows a group has on average and how many tiles of 64 x 256 there would be (256 of them, four to a
-    // compute unit, are a round).  us, 32 x 128 against 64 x 256, 64 groups, K x N: tokens in bf16, 48 a group, 768 x 3072 27.3 / 22.6, 64 a group,
-    // 1024 x 1024 16.6 / 18.0, 3072 x 768 29.8 / 41.6, 128 a group 48.9 / 44.8; in 4 bits, 24 a group, 768 x 3072 16.2 / 15.7, 32 a
-    // group, 4096 x 1024, Zipf sizes, 28.3 / 29.7, 64 a group 34.2 / 30.8.
-    const int64_t mean = a.M / a.groups, wide = (a.M / 64 + a.groups / 2) * (int64_t)((a.N + 255) / 256);
-    if (X4 ? mean <= 16 || wide < 320 : mean <= 32 || wide < 480) return launch_shape<X4, 1, 1, X4 ? 2 : 4, X4 ? 2 : 4, X4 ? 5 : 6, Y>(a, st);
-    // 128 x 256 for long rows in 4 bits: 256 tokens for each of 128 groups, 4096 x 1024, 109 us against 122; with rows of 768 three stages
-    // are a tile's whole sum, and two workgroups to a compute unit too few (256 a group, 64 groups, 43.0 against 38.1).
-    if constexpr (X4)
-        if (a.K >= 2048 && mean >= 192) return launch_shape<X4, 4, 2, 2, 1, 2, Y>(a, st);
+    case MxTiles::rows32: return launch_shape<X4, 1, 1, X4 ? 2 : 4, X4 ? 2 : 4, X4 ? 5 : 6, Y>(a, st);
+    case MxTiles::rows128:
+        if constexpr (X4) return launch_shape<X4, 4, 2, 2, 1, 2, Y>(a, st);
+        break;                                                 // 4 bits alone have it
+    case MxTiles::rows64: break;
+    }
     return launch_shape<X4, 2, 2, 2, X4 ? 1 : 2, 4, Y>(a, st);
 }
 
