@@ -430,7 +430,8 @@ int sida_mx_quantize(const void *x_dev, int32_t x_type, int64_t rows, int32_t co
  *   x_dev       x_type SIDA_BF16: [M, K], rows ldx values apart (ldx >= K), 16-byte aligned, ldx a multiple of 8
  *               x_type SIDA_MXFP4: codes in SIDA_MX_ROWS layout (16-byte aligned, ldx = K), x_scales_dev their scales (8-byte aligned)
  *   codes_dev   [groups] matrices [N, K] in SIDA_MX_TILES layout, sida_mx_codes_bytes(N, K, SIDA_MX_TILES) bytes apart (16-byte aligned)
- *   scales_dev  their scales, likewise (4-byte aligned)
+ *   scales_dev  their scales, likewise (4-byte aligned).  sida_mx_quantize writes powers of two up to 2^125 (byte 252).  Of larger ones
+ *               the weights of 2^128 and more count as infinite where the tokens are bf16, which holds no such numbers.
  *   offsets_dev int32 [groups+1], ascending, 0 .. M.  Values outside are taken as the nearest of 0 and M, a group whose end
  *               is before its start as empty; rows of y that belong to no group keep what they hold (with offsets that do not
                ascend, which of the rows are computed is not defined; no others are touched).  NULL with one group: all rows.

@@ -111,7 +111,8 @@ __device__ __forceinline__ Placed place(const MxArgs &a, int n_tiles)
     return Placed{__builtin_amdgcn_readlane(group, owner), __builtin_amdgcn_readlane(row0, owner), __builtin_amdgcn_readlane(rows, owner), id % n_tiles};
 }
 
-// Eight codes times their power of two, exact in bf16.
+// Eight codes times their power of two, exact in bf16, which has room for 1/2 * 2^-127 as well; infinite from 2^128 on (powers of two above
+// 2^125, which rounding to MXFP4 does not give).
 __device__ __forceinline__ bf16x8 decode(uint32_t c, float s)
 {
     bf16x8 o;

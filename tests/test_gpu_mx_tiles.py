@@ -150,6 +150,38 @@ def test_first_and_last_powers(size, byte):
     assert np.array_equal(y.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("byte", [253, 254])
+@pytest.mark.parametrize("size", EACH, ids=repr)
+def test_powers_beyond(size, byte):
+    """Powers of two that only other programs' codes have.  Weights of 2^128 and more: infinite against bf16 tokens, exact against codes."""
+    ex = size.experts(7)
+    ex.codes[:, ::2] &= 0xB                                            # every other column of results has small codes only
+    ex.scales[:] = byte
+    ex.upload()
+    if not size.x4:
+        assert all((np.abs(w[1::2]) >= 2.0 ** 128).any() for w in ex.w)
+        ex.w = [np.where(np.abs(w) >= 2.0 ** 128, np.copysign(np.inf, w), w) for w in ex.w]
+    g = np.random.default_rng(byte)
+    M = size.M
+    at, e = g.integers(0, size.K, M), g.integers(-126, -3, M)
+    if size.x4:
+        codes = np.zeros((M, size.K), np.uint8)
+        codes[np.arange(M), at] = g.integers(1, 16, M)
+        scales = np.repeat((e + 127).astype(np.uint8)[:, None], size.K // 32, 1)
+        x = mx.values(codes, scales)
+        xd, xs = (dev(v) for v in mx.pack_rows(codes, scales))
+    else:
+        x = np.zeros((M, size.K))
+        x[np.arange(M), at] = np.ldexp(g.choice([-1.5, -1.0, 1.0, 1.75], M), e)
+        xd, xs = dev(x, torch.bfloat16), None
+    offsets = bounds(size.counts)
+    y = torch.empty((M, size.N), device=DEV)
+    sm.mx_gemm(xd, xs, ex.dev_codes, ex.dev_scales, dev(offsets.astype(np.int32)), y, stream())
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = product(ex, x, offsets).astype(np.float32)
+    assert np.array_equal(y.cpu().numpy(), want, equal_nan=True)
+
+
 # Weights N(0, 0.02) and tokens N(0, 1), rounded by the library.  An fp32 sum of K products is off by at most K 2^-23 times the sum of their
 # magnitudes (each addition rounds, or cuts, a partial sum of at most that size).
 @pytest.mark.parametrize("size", EACH, ids=repr)
