@@ -425,7 +425,8 @@ int sida_mx_quantize(const void *x_dev, int32_t x_type, int64_t rows, int32_t co
 
 /* Grouped product of token rows with experts in 4 bits: rows offsets[g] .. offsets[g+1]-1 belong to expert g,
  *     y[r,:] = W_g x[r,:]        (relu != 0: negative results, -0 among them, become 0)
- * exact products, sums in fp32, one rounding (to nearest even) where y is bf16.  The rows of a sorted batch, as sida_dispatch
+ * exact products, sums in fp32, one rounding (to nearest even) where y is bf16.  The same call gives the same bits; small products add in
+ * another order than large ones (by M, groups, N and K), so that a row's last bits may depend on the batch it is in.  The rows of a sorted batch, as sida_dispatch
  * leaves them.  One group is a plain product; a single row streams one matrix.
  *   x_dev       x_type SIDA_BF16: [M, K], rows ldx values apart (ldx >= K), 16-byte aligned, ldx a multiple of 8
  *               x_type SIDA_MXFP4: codes in SIDA_MX_ROWS layout (16-byte aligned, ldx = K), x_scales_dev their scales (8-byte aligned)
@@ -434,7 +435,7 @@ int sida_mx_quantize(const void *x_dev, int32_t x_type, int64_t rows, int32_t co
  *               the weights of 2^128 and more count as infinite where the tokens are bf16, which holds no such numbers.
  *   offsets_dev int32 [groups+1], ascending, 0 .. M.  Values outside are taken as the nearest of 0 and M, a group whose end
  *               is before its start as empty; rows of y that belong to no group keep what they hold (with offsets that do not
-               ascend, which of the rows are computed is not defined; no others are touched).  NULL with one group: all rows.
+ *             ascend, which of the rows are computed is not defined; no others are touched).  NULL with one group: all rows.
  *   y_dev       y_type SIDA_BF16 or SIDA_FP32: [M, N], rows ldy values apart (ldy >= N), at any address of such a value;
  *               faster where all rows begin and end on 16-byte boundaries, and on 4-byte ones in bf16.
  * Limits: 1 <= groups <= SIDA_MAX_E; K as cols above; 1 <= N <= 65536; 0 <= M <= 2^24, M * N <= 2^35; ldx, ldy < 2^24. */

@@ -10,9 +10,10 @@
 // and are read by one wavefront only; the token rows, which all four wavefronts of a workgroup need, go through LDS.
 //
 // What bounds it.  Few tokens for each expert: the experts' bytes (128 tokens in bf16, 50 experts of 768 x 3072 in use, 12.3 us for 66 MB,
-// 5.3 TB/s; 1111 of 64 experts, 3072 x 768, 17.2 us for 87 MB).  Many: matrix cores and the way from L2 to the compute unit in turns, each
-// of them busy about half of the time (16384 tokens, 128 experts of 768 x 3072: 86 to 94 us, 77 GFLOP, 0.85 PFLOP/s, 48% of the matrix cores' cycles;
-// 32768 in 4 bits, 4096 x 1024: 107 to 112 us, 2.5 PFLOP/s for 406 MB); one matrix, 16384 x 4096 x 4096, 1.36 PFLOP/s in bf16, 2.95 in 4 bits.
+// 5.3 TB/s; 1111 of 64 experts, 3072 x 768, 17.2 us for 87 MB).  Many: neither matrix cores nor loads, but that they overlap only in part.  16384
+// tokens, 128 experts of 768 x 3072, bf16: 86 to 94 us, 77 GFLOP, 0.85 PFLOP/s, 48% of the matrix cores' cycles (an earlier build took 70 us
+// for the products and 69 for the data).  32768 in 4 bits, 4096 x 1024: 107 to 112 us, 2.5 PFLOP/s for 406 MB, 27% (loads alone 68 us in an earlier
+// build: weights are one stage ahead and there are two wavefronts to a SIMD).  One matrix, 16384 x 4096 x 4096, 1.36 PFLOP/s in bf16, 2.95 in 4 bits.
 #include <hip/hip_runtime.h>
 
 #include <cstddef>

@@ -8,9 +8,12 @@
 // pass reads them once.  exp(v - m) is 2^((v - m) log2 e), the difference first: m log2 e on its own would overflow where all logits
 // are the type's lowest value.
 //
-// Small batches are bound by the launch.  Large ones, forward, by the vector instructions, about 10 for a logit and 6 more for each
-// expert a token has (32768 tokens of 256 fp32 logits, 3 experts each: 14 us for 34 MB, and 4.6 us for the sums; 107351 of 239, 8
-// each: 56 us for 110 MB).  Backward, about 14 for a logit, by bytes: 262144 of 128 fp32 logits, 270 MB in 45 us, 6.0 TB/s.
+// Small batches are bound by the launch.  Large ones, forward: about 10 vector instructions for a logit and 6 more for each expert a token
+// has, which are most of the time where a token has many (107351 tokens of 239 bf16 logits, 8 experts each: 54 us for 58 MB; 26.5 million
+// instructions, 43 us if each SIMD issues one in four cycles at 2.4 GHz), and about half of it otherwise, the rest being loads and exchanges that
+// are waited for with two rounds of tokens to a workgroup (32768 of 256 fp32 logits, 3 each: 13 us for 34 MB, 6.8 us of instructions;
+// 40000 of 129 bf16 logits, 1 each: 10.5 and 5.8).  The sums of the workgroups are another 4.2 to 4.7 us.  Backward, about 14 for a logit, by
+// bytes: 262144 of 128 fp32 logits, 270 MB in 47 us, 5.7 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
