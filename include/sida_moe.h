@@ -485,6 +485,82 @@ int sida_route_backward(const sida_route_config *cfg, const void *logits_dev, in
                         const int32_t *ids_dev, const int32_t *counts_dev, const float *d_gates_dev, const float *d_loss_dev,
                         void *d_logits_dev, int64_t ld_d, void *stream);
 
+/* ---- tokens to their experts and back ----------------------------------------------------------
+ * A routed layer around experts that are kept as plain bf16 matrices, for training and for serving: sida_route, then sort, rows, products
+ * (below) and sum; and the way back.  No context is needed; the calls are asynchronous on `stream`, allocate nothing and may be captured into a HIP graph.
+ * Pair p = t * top_k + j is token t's j-th expert.  It takes part where its id lies within [0,E) and its gate (where gates are given) is not 0: a
+ * router's gates are 0 where a token is masked, and a caller without one gives ids of -1.
+ * T tokens, E <= SIDA_MAX_E, top_k <= SIDA_MAX_TOP_K, T * top_k < 2^31. */
+
+/* Sorts the pairs by expert, those of one expert in their order:
+ *     offsets_dev int32 [E+1]      exclusive sums of the pairs per expert; offsets[E] is how many take part
+ *     places_dev  int32 [T,top_k]  the pair's row in expert order, -1 without a part
+ * ids_dev int32 [T,top_k]; gates_dev NULL or fp32 [T,top_k] (0 and -0: no part; NaN takes part); workspace_dev 4-byte aligned,
+ * >= sida_expert_sort_workspace_bytes(E, top_k, T), scratch of this call alone until it is done. */
+size_t sida_expert_sort_workspace_bytes(int32_t E, int32_t top_k, int32_t T);  /* 0 on bad arguments */
+int sida_expert_sort(int32_t E, int32_t top_k, const int32_t *ids_dev, const float *gates_dev, int32_t T, int32_t *offsets_dev,
+                     int32_t *places_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Rows between token order [T, d] and expert order [M, d], all of one type (SIDA_BF16 or SIDA_FP32), sums in fp32, one rounding.
+ * Consecutive rows are `ld` values apart (ld >= d, < 2^24), at any address of such a value; faster where all rows begin and end on 16-byte boundaries.
+ * places_dev is what sida_expert_sort leaves: no two are alike, and one outside [0,M) stands for a pair without a part (M >= T * top_k
+ * always suffices).  1 <= d <= 65536, 0 <= M < 2^31. */
+typedef struct sida_expert_rows_config {
+    int32_t T, top_k;     /* tokens, experts per token           */
+    int32_t M, d;         /* expert rows, values of a row        */
+    int32_t type;         /* SIDA_BF16 or SIDA_FP32              */
+} sida_expert_rows_config;
+/* rows[places[t,j]] = x[t].  Rows that are no pair's place keep what they hold. */
+int sida_expert_rows(const sida_expert_rows_config *cfg, const void *x_dev, int64_t ld_x, const int32_t *places_dev, void *rows_dev,
+                     int64_t ld_rows, void *stream);
+/* y[t] = residual[t] + sum_j gates[t,j] rows[places[t,j]], terms in the order of j, over the pairs that take part.  gates_dev NULL: ones, which is
+ * the gradient of sida_expert_rows.  residual_dev NULL: none; it may be y (with ld_res = ld_y).  Rows without a pair are not read. */
+int sida_expert_sum(const sida_expert_rows_config *cfg, const void *rows_dev, int64_t ld_rows, const int32_t *places_dev, const float *gates_dev,
+                    const void *residual_dev, int64_t ld_res, void *y_dev, int64_t ld_y, void *stream);
+/* The gradient of sida_expert_sum from dy [T, d] (that of the residual is dy):
+ *     d_rows[places[t,j]] = gates[t,j] dy[t]          other rows keep what they hold
+ *     d_gates[t,j] = dy[t] . rows[places[t,j]]        0 without a part
+ * d_gates_dev fp32 [T,top_k], or NULL, and then rows_dev is not read and may be NULL.  d_rows may be rows (with ld_d = ld_rows). */
+int sida_expert_sum_backward(const sida_expert_rows_config *cfg, const void *dy_dev, int64_t ld_dy, const void *rows_dev, int64_t ld_rows,
+                             const int32_t *places_dev, const float *gates_dev, void *d_rows_dev, int64_t ld_d, float *d_gates_dev, void *stream);
+
+/* ---- products of plain bf16 experts, forward and backward -----------------------------------------
+ * Rows offsets[g] .. offsets[g+1]-1 belong to expert g, whose matrix W_g is bf16 [N, K] and follows that of expert g-1; one group is a plain
+ * linear layer.  Sums in fp32 in a fixed order, one rounding (to nearest even) for each result; the same call gives the same bits (sizes choose
+ * among orders, so that a row's last bits may depend on the batch it is in).
+ * Activations: v, max(v, 0), GELU in its form with tanh, v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))), and SiLU, v / (1 + exp(-v)).
+ * All matrices are row-major, 16-byte aligned, with consecutive rows a multiple of 16 bytes apart; N and K are multiples of 8.
+ *   offsets_dev int32 [groups+1], ascending, 0 .. M (values outside are taken as the nearest of 0 and M, a group whose end is before its start as empty;
+ *               with offsets that do not ascend, which rows are computed is not defined; no others are touched).  Rows of no group
+ *               keep what they hold, and are not read.  NULL with one group: all rows.
+ * Limits: 1 <= groups <= SIDA_MAX_E; N, K in 8 .. 65536, N * K <= 2^30, groups * N * K <= 2^36; 0 <= M <= 2^24; M * N and M * K <= 2^35; rows at most 2^22 values apart. */
+enum { SIDA_ACT_NONE = 0, SIDA_ACT_RELU = 1, SIDA_ACT_GELU = 2, SIDA_ACT_SILU = 3 };
+typedef struct sida_expert_gemm_config {
+    int32_t groups;       /* experts                                            */
+    int32_t N, K;         /* rows and columns of an expert's matrix             */
+    int32_t out_type;     /* of the result (and residual): SIDA_BF16, SIDA_FP32 */
+    int32_t activation;   /* SIDA_ACT_*; SIDA_ACT_NONE for the weights' gradient */
+} sida_expert_gemm_config;
+/* v = W_g x[r] + bias_g,  y[r] = act(v) + residual[r].
+ *   x_dev bf16 [M, K], w_dev bf16 [groups, N, K], bias_dev NULL or fp32 [groups, N] (16-byte aligned), y_dev out_type [M, N]
+ *   pre_dev      NULL, or bf16 [M, N]: v, for the backward pass (with SIDA_ACT_RELU and no residual y in bf16 serves as well)
+ *   residual_dev NULL, or out_type [M, N]; may be y (with ld_res = ldy) */
+int sida_expert_gemm(const sida_expert_gemm_config *cfg, const void *x_dev, int64_t ldx, int32_t M, const void *w_dev, const int32_t *offsets_dev,
+                     const float *bias_dev, void *pre_dev, int64_t ld_pre, const void *residual_dev, int64_t ld_res, void *y_dev, int64_t ldy,
+                     void *stream);
+/* The gradient of the rows, and of what an activation has made them from:  dx[r] = (W_g^T dy[r]) act'(pre[r]).
+ *   dy_dev bf16 [M, N], w_dev as above, dx_dev out_type [M, K]
+ *   pre_dev      bf16 [M, K], the values in front of the activation that gave x; NULL with SIDA_ACT_NONE only.  May be dx where out_type is
+ *                SIDA_BF16 (with ld_pre = ld_dx).  max(v, 0) has slope 0 at 0. */
+int sida_expert_gemm_input(const sida_expert_gemm_config *cfg, const void *dy_dev, int64_t ld_dy, int32_t M, const void *w_dev,
+                           const int32_t *offsets_dev, const void *pre_dev, int64_t ld_pre, void *dx_dev, int64_t ld_dx, void *stream);
+/* The gradients of matrices and biases:  dW_g = sum_r dy[r] x[r]^T,  dbias_g = sum_r dy[r]  over the rows r of group g; 0 for a group without rows.
+ *   dy_dev bf16 [M, N], x_dev bf16 [M, K], dw_dev out_type [groups, N, K], d_bias_dev NULL or fp32 [groups, N]
+ *   workspace_dev  16-byte aligned, >= sida_expert_gemm_weights_workspace_bytes(cfg, M), scratch of this call alone until it is done (NULL where that is 0) */
+size_t sida_expert_gemm_weights_workspace_bytes(const sida_expert_gemm_config *cfg, int32_t M);
+int sida_expert_gemm_weights(const sida_expert_gemm_config *cfg, const void *dy_dev, int64_t ld_dy, const void *x_dev, int64_t ldx, int32_t M,
+                             const int32_t *offsets_dev, void *dw_dev, float *d_bias_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* Inspection: the order in which a grouped-GEMM launch walks its output tiles.  For a launch over
  * m_tiles token tiles (the first m_tall of them belonging to experts with more than one tile) and
  * n_tiles_n weight-row tiles, fills token_tile[t], weight_tile[t] for t = 0 .. m_tiles*n_tiles_n-1

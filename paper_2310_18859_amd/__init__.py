@@ -8,4 +8,6 @@ from .binding import (  # noqa: F401
     hash_forward, hash_forward_static,
     BF16, FP32, MXFP4, MX_ROWS, MX_TILES, SidaMxGemmConfig, SidaRouteConfig, mx_codes_bytes, mx_scales_bytes, mx_quantize, mx_gemm,
     route_workspace_bytes, route, route_backward,
+    ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, SidaExpertRowsConfig, SidaExpertGemmConfig, expert_sort_workspace_bytes, expert_sort, expert_rows,
+    expert_sum, expert_sum_backward, expert_gemm, expert_gemm_input, expert_gemm_weights_workspace_bytes, expert_gemm_weights,
 )

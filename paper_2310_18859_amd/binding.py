@@ -12,6 +12,7 @@ EAGAIN, ECLOSED = -6, -7
 DEBUG_CHECK_IDS, DEBUG_POISON_SLOTS = 1, 2
 BF16, FP32, MXFP4 = 0, 1, 2
 MX_ROWS, MX_TILES = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 K_NAMES = ("sort", "gather", "gemm1", "gemm2", "combine", "copy")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -59,6 +60,14 @@ class SidaRouteConfig(C.Structure):
 class WsLayout(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in
                 ("counts", "offsets", "block_hist", "perm", "inv", "x_perm", "h", "y_perm", "tiles", "sink", "gate_perm", "total")]
+
+
+class SidaExpertRowsConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "top_k", "M", "d", "type")]
+
+
+class SidaExpertGemmConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("groups", "N", "K", "out_type", "activation")]
 
 
 _LIB = None
@@ -124,6 +133,15 @@ def lib():
         "sida_route_workspace_bytes": (sz, [C.POINTER(SidaRouteConfig), i32]),
         "sida_route": (C.c_int, [C.POINTER(SidaRouteConfig), vp, C.c_int64, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
         "sida_route_backward": (C.c_int, [C.POINTER(SidaRouteConfig), vp, C.c_int64, i32, vp, vp, vp, vp, vp, vp, C.c_int64, vp]),
+        "sida_expert_sort_workspace_bytes": (sz, [i32, i32, i32]),
+        "sida_expert_sort": (C.c_int, [i32, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
+        "sida_expert_rows": (C.c_int, [C.POINTER(SidaExpertRowsConfig), vp, C.c_int64, vp, vp, C.c_int64, vp]),
+        "sida_expert_sum": (C.c_int, [C.POINTER(SidaExpertRowsConfig), vp, C.c_int64, vp, vp, vp, C.c_int64, vp, C.c_int64, vp]),
+        "sida_expert_sum_backward": (C.c_int, [C.POINTER(SidaExpertRowsConfig), vp, C.c_int64, vp, C.c_int64, vp, vp, vp, C.c_int64, vp, vp]),
+        "sida_expert_gemm": (C.c_int, [C.POINTER(SidaExpertGemmConfig), vp, C.c_int64, i32, vp, vp, vp, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp]),
+        "sida_expert_gemm_input": (C.c_int, [C.POINTER(SidaExpertGemmConfig), vp, C.c_int64, i32, vp, vp, vp, C.c_int64, vp, C.c_int64, vp]),
+        "sida_expert_gemm_weights_workspace_bytes": (sz, [C.POINTER(SidaExpertGemmConfig), i32]),
+        "sida_expert_gemm_weights": (C.c_int, [C.POINTER(SidaExpertGemmConfig), vp, C.c_int64, vp, C.c_int64, i32, vp, vp, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -342,6 +360,172 @@ def route_backward(logits, ids, counts, d_logits, stream, d_gates=None, d_loss=N
         None if d_loss is None else _flat(d_loss, 1, "fp32", "d_loss"), d_logits.data_ptr(), ld_d, _stream(stream))
     if rc:
         raise SidaError(rc, "sida_route_backward")
+
+
+# ---- plain bf16 experts: tokens to them and back, their products, and the gradients.
+@functools.lru_cache(maxsize=1024)
+def _expert_rows_config(*fields):
+    _need_int32(*fields)
+    cfg = SidaExpertRowsConfig(*fields)
+    return cfg, C.byref(cfg)
+
+
+@functools.lru_cache(maxsize=1024)
+def _expert_gemm_config(*fields):
+    _need_int32(*fields)
+    cfg = SidaExpertGemmConfig(*fields)
+    return cfg, C.byref(cfg)
+
+
+def _pairs(t, kind: str, what: str):
+    """(tokens, experts per token) of a contiguous matrix of a type on the GPU."""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype not in _KINDS[kind] or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: a contiguous matrix [tokens, experts per token] of {kind} values on the GPU is needed")
+    return shape
+
+
+def expert_sort_workspace_bytes(E: int, top_k: int, T: int) -> int:
+    return lib().sida_expert_sort_workspace_bytes(E, top_k, T) if _is_int32(E, top_k, T) else 0
+
+
+def expert_sort(ids, offsets, places, workspace, stream, gates=None):
+    """ids: int32 [T, k]; offsets: int32 [E + 1], written; places: int32 [T, k], written; workspace: uint8, expert_sort_workspace_bytes of it;
+    gates: fp32 [T, k] or None (pairs whose gate is 0 take no part, nor do those whose id is not one of the E experts')."""
+    T, k = _pairs(ids, "int32", "ids")
+    E = offsets.numel() - 1
+    _need_int32(T, E)
+    rc = (_LIB or lib()).sida_expert_sort(
+        E, k, ids.data_ptr(), None if gates is None else _flat(gates, T * k, "fp32", "gates"), T, _flat(offsets, 1, "int32", "offsets"),
+        _flat(places, T * k, "int32", "places"), _flat(workspace, 0, "uint8", "workspace"), workspace.numel(), _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_expert_sort")
+
+
+def _tokens_and_rows(tokens, rows, places, what: str):
+    """(config, tokens' ld, rows' ld) of a matrix in token order and one in expert order."""
+    n, d, ld = _rows(tokens, what)
+    M, d_rows, ld_rows = _rows(rows, "rows")
+    T, k = _pairs(places, "int32", "places")
+    kind = _type(tokens)
+    if n != T or d_rows != d or _KINDS[rows.dtype] != kind:
+        raise ValueError(f"{what} and rows: [{T}, d] and [rows, d] of one type are needed, not {list(tokens.shape)} of {tokens.dtype} and "
+                         f"{list(rows.shape)} of {rows.dtype}")
+    return _expert_rows_config(T, k, M, d, kind)[1], T, k, d, kind, ld, ld_rows
+
+
+def _like(t, rows, cols, kind, what):
+    """(address, ld) of a matrix of that shape and type, (None, 0) for None."""
+    if t is None:
+        return None, 0
+    n, d, ld = _rows(t, what)
+    if n != rows or d != cols or _KINDS[t.dtype] != kind:
+        raise ValueError(f"{what}: [{rows}, {cols}] of {'bf16' if kind == BF16 else 'fp32'} is needed, not {list(t.shape)} of {t.dtype}")
+    return t.data_ptr(), ld
+
+
+def expert_rows(x, places, rows, stream):
+    """x: bf16 or fp32 [T, d]; places: int32 [T, k]; rows: as x, [M, d], written where a pair has its place."""
+    cfg, _, _, _, _, ld, ld_rows = _tokens_and_rows(x, rows, places, "x")
+    rc = (_LIB or lib()).sida_expert_rows(cfg, x.data_ptr(), ld, places.data_ptr(), rows.data_ptr(), ld_rows, _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_expert_rows")
+
+
+def expert_sum(rows, places, y, stream, gates=None, residual=None):
+    """rows: bf16 or fp32 [M, d]; places: int32 [T, k]; y: as rows, [T, d], written; gates: fp32 [T, k] or None (ones, which gives the gradient of
+    expert_rows); residual: as y, or None."""
+    cfg, T, k, d, kind, ld, ld_rows = _tokens_and_rows(y, rows, places, "y")
+    res, ld_res = _like(residual, T, d, kind, "residual")
+    rc = (_LIB or lib()).sida_expert_sum(cfg, rows.data_ptr(), ld_rows, places.data_ptr(), None if gates is None else _flat(gates, T * k, "fp32", "gates"),
+                                         res, ld_res, y.data_ptr(), ld, _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_expert_sum")
+
+
+def expert_sum_backward(dy, rows, places, d_rows, stream, gates=None, d_gates=None):
+    """dy: bf16 or fp32 [T, d]; rows: as dy, [M, d], or None without d_gates; d_rows: as dy, [M, d], written where a pair has its place; gates: fp32
+    [T, k] or None (ones); d_gates: fp32 [T, k], written, or None."""
+    cfg, T, k, d, kind, ld, ld_d = _tokens_and_rows(dy, d_rows, places, "dy")
+    if d_gates is not None and rows is None:
+        raise ValueError("rows: needed for d_gates")
+    at, ld_rows = _like(rows, d_rows.shape[0], d, kind, "rows")
+    rc = (_LIB or lib()).sida_expert_sum_backward(
+        cfg, dy.data_ptr(), ld, at, ld_rows, places.data_ptr(), None if gates is None else _flat(gates, T * k, "fp32", "gates"), d_rows.data_ptr(),
+        ld_d, None if d_gates is None else _flat(d_gates, T * k, "fp32", "d_gates"), _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_expert_sum_backward")
+
+
+def _experts(w, offsets, what: str):
+    """(groups, N, K) of the experts' matrices, one after the other; [N, K] is one group."""
+    shape = w.shape
+    groups = 1 if offsets is None else offsets.numel() - 1
+    if len(shape) not in (2, 3) or not w.is_contiguous() or not w.is_cuda or (shape[0] if len(shape) == 3 else 1) != groups:
+        raise ValueError(f"{what}: contiguous matrices [{groups}, N, K] on the GPU are needed, not {list(shape)}")
+    return groups, shape[-2], shape[-1]
+
+
+def _offsets(offsets):
+    return None if offsets is None else _flat(offsets, 1, "int32", "offsets")
+
+
+def expert_gemm(x, w, offsets, y, stream, bias=None, activation=ACT_NONE, pre=None, residual=None):
+    """x: bf16 [M, K]; w: bf16 [groups, N, K]; offsets: int32 [groups + 1], or None for one group; y: bf16 or fp32 [M, N], written; bias: fp32
+    [groups, N] or None; activation: ACT_NONE, ACT_RELU, ACT_GELU or ACT_SILU; pre: bf16 [M, N], written with what the activation is given, or None;
+    residual: as y, or None."""
+    groups, N, K = _experts(w, offsets, "w")
+    M, cols, ldx = _rows(x, "x")
+    if cols != K or _type(x) != BF16 or _type(w) != BF16:
+        raise ValueError(f"x and w: bf16 [M, {K}] and [groups, N, {K}] are needed, not {list(x.shape)} of {x.dtype} and {list(w.shape)} of {w.dtype}")
+    kind = _type(y)
+    to, ldy = _like(y, M, N, kind, "y")
+    at, ld_pre = _like(pre, M, N, BF16, "pre")
+    res, ld_res = _like(residual, M, N, kind, "residual")
+    _need_int32(M)
+    rc = (_LIB or lib()).sida_expert_gemm(
+        _expert_gemm_config(groups, N, K, kind, activation)[1], x.data_ptr(), ldx, M, w.data_ptr(), _offsets(offsets),
+        None if bias is None else _flat(bias, groups * N, "fp32", "bias"), at, ld_pre, res, ld_res, to, ldy, _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_expert_gemm")
+
+
+def expert_gemm_input(dy, w, offsets, dx, stream, pre=None, activation=ACT_NONE):
+    """dy: bf16 [M, N]; w: bf16 [groups, N, K]; offsets: int32 [groups + 1], or None for one group; dx: bf16 or fp32 [M, K], written; pre: bf16
+    [M, K], what the activation in front of the product was given, or None without one."""
+    groups, N, K = _experts(w, offsets, "w")
+    M, cols, ld_dy = _rows(dy, "dy")
+    if cols != N or _type(dy) != BF16 or _type(w) != BF16:
+        raise ValueError(f"dy and w: bf16 [M, {N}] and [groups, {N}, K] are needed, not {list(dy.shape)} of {dy.dtype} and {list(w.shape)} of {w.dtype}")
+    kind = _type(dx)
+    to, ld_dx = _like(dx, M, K, kind, "dx")
+    at, ld_pre = _like(pre, M, K, BF16, "pre")
+    _need_int32(M)
+    rc = (_LIB or lib()).sida_expert_gemm_input(_expert_gemm_config(groups, N, K, kind, activation)[1], dy.data_ptr(), ld_dy, M, w.data_ptr(),
+                                                _offsets(offsets), at, ld_pre, to, ld_dx, _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_expert_gemm_input")
+
+
+def expert_gemm_weights_workspace_bytes(cfg: SidaExpertGemmConfig, M: int) -> int:
+    return lib().sida_expert_gemm_weights_workspace_bytes(C.byref(cfg), M) if _is_int32(M) else 0
+
+
+def expert_gemm_weights(dy, x, offsets, dw, workspace, stream, d_bias=None):
+    """dy: bf16 [M, N]; x: bf16 [M, K]; offsets: int32 [groups + 1], or None for one group; dw: bf16 or fp32 [groups, N, K], written; workspace: uint8,
+    expert_gemm_weights_workspace_bytes of it; d_bias: fp32 [groups, N], written, or None."""
+    groups, N, K = _experts(dw, offsets, "dw")
+    M, n, ld_dy = _rows(dy, "dy")
+    rows, k, ldx = _rows(x, "x")
+    if n != N or k != K or rows != M or _type(dy) != BF16 or _type(x) != BF16:
+        raise ValueError(f"dy and x: bf16 [M, {N}] and [M, {K}] are needed, not {list(dy.shape)} of {dy.dtype} and {list(x.shape)} of {x.dtype}")
+    _need_int32(M)
+    rc = (_LIB or lib()).sida_expert_gemm_weights(
+        _expert_gemm_config(groups, N, K, _type(dw), ACT_NONE)[1], dy.data_ptr(), ld_dy, x.data_ptr(), ldx, M, _offsets(offsets), dw.data_ptr(),
+        None if d_bias is None else _flat(d_bias, groups * N, "fp32", "d_bias"), _flat(workspace, 0, "uint8", "workspace"), workspace.numel(),
+        _stream(stream))
+    if rc:
+        raise SidaError(rc, "sida_expert_gemm_weights")
 
 
 def streams_create(copy_cus: int):

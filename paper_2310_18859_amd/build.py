@@ -10,8 +10,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsida_moe.so")
 SOURCES = ["api.cpp", "plan.cpp", "sort_gather.hip", "grouped_ffn.hip", "combine.hip", "prefetch.hip", "hash_fn.hip", "debug.hip",
-           "api_ops.cpp", "mx_quant.hip", "mx_gemm.hip", "route.hip"]
-HEADERS = ["ctx.h", "kernels.h", "tile_order.h", "handover.h", "past_end.h", "lds_grant.h", "tile_rule.h", "heads_walk.h", "mx_rule.h"]
+           "api_ops.cpp", "mx_quant.hip", "mx_gemm.hip", "route.hip", "expert_rows.hip", "expert_gemm.hip"]
+HEADERS = ["ctx.h", "kernels.h", "tile_order.h", "handover.h", "past_end.h", "lds_grant.h", "tile_rule.h", "heads_walk.h", "mx_rule.h", "expert_rule.h"]
 
 
 def _newest_source() -> float:

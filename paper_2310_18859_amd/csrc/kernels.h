@@ -156,4 +156,30 @@ int launch_route(const RouteShape &s, const void *logits, int64_t ld, int32_t T,
 int launch_route_backward(const RouteShape &s, const void *logits, int64_t ld, int32_t T, const uint8_t *mask, const int32_t *ids,
                           const int32_t *counts, const float *d_gates, const float *d_loss, void *d_logits, int64_t ld_d, hipStream_t st);
 
+// Tokens to their experts and back (expert_rows.hip); the arguments are those of the C calls, checked.
+int launch_expert_sort(const int32_t *ids, const float *gates, int64_t pairs, int32_t E, int32_t *offsets, int32_t *places, void *ws, hipStream_t st);
+struct ExpertRowsShape {
+    int32_t T, k, M, d;          // tokens, experts of each, expert rows, values of a row
+    bool fp32;
+};
+int launch_expert_rows(const ExpertRowsShape &s, const void *x, int64_t ld_x, const int32_t *places, void *rows, int64_t ld_rows, hipStream_t st);
+int launch_expert_sum(const ExpertRowsShape &s, const void *rows, int64_t ld_rows, const int32_t *places, const float *gates, const void *residual,
+                      int64_t ld_res, void *y, int64_t ld_y, hipStream_t st);
+int launch_expert_sum_backward(const ExpertRowsShape &s, const void *dy, int64_t ld_dy, const void *rows, int64_t ld_rows, const int32_t *places,
+                               const float *gates, void *d_rows, int64_t ld_d, float *d_gates, hipStream_t st);
+
+// Plain bf16 experts' products (expert_gemm.hip).
+enum { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+struct ExpertGemmShape {
+    int32_t groups, N, K;
+    bool out32;
+    int32_t activation;
+};
+int launch_expert_gemm(const ExpertGemmShape &s, const void *x, int64_t ldx, int32_t M, const void *w, const int32_t *offsets, const float *bias,
+                       void *pre, int64_t ld_pre, const void *residual, int64_t ld_res, void *y, int64_t ldy, hipStream_t st);
+int launch_expert_gemm_input(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, int32_t M, const void *w, const int32_t *offsets, const void *pre,
+                             int64_t ld_pre, void *dx, int64_t ld_dx, hipStream_t st);
+int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, int32_t M, const int32_t *offsets,
+                               void *dw, float *d_bias, void *ws, hipStream_t st);
+
 }  // namespace sida
