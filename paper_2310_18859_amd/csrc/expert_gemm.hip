@@ -47,99 +47,201 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, ui
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
 }
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t offset, void *dst)
+// 16 bytes a lane straight into LDS: lane i's land at dst + 16 i.  Written out, because the compiler waits for all that it knows to be on its way to LDS
+// in front of each transposing read (8192 cubed, the input's gradient: 1089 us against 947); it has no register as its result, and waits that the compiler
+// counts without it wait longer, never shorter.  The pauses: a scalar register written by a vector instruction, or M0, is not there at once.
+__device__ __forceinline__ i32x4 lds_source(const char *base, uint32_t bytes)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 16, (int)offset, 0, 0, 0);
+    return i32x4{(int)(uint32_t)(uint64_t)base, (int)((uint64_t)base >> 32 & 0xffff), (int)bytes, 0x00020000};
+}
+__device__ __forceinline__ void load_to_lds(i32x4 source, uint32_t offset, uint32_t dst)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(offset), "s"(source) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// A uniform value that the compiler cannot see through: it makes one copy of the code that depends on it, not one for each value.
+__device__ __forceinline__ int hidden(int v)
+{
+    v = __builtin_amdgcn_readfirstlane(v);
+    asm("" : "+s"(v));
+    return v;
+}
+// What is the same in all lanes, in scalar registers whatever the compiler makes of where it comes from: a descriptor out of vector registers
+// costs a loop around its access.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const char *uniform(const char *p)
+{
+    const uint64_t v = (uint64_t)p;
+    return (const char *)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+// A value that the compiler cannot see through: what follows from it is worked out where it is used, rather than held in registers all the time.
+__device__ __forceinline__ int anew(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
 // A descriptor's records, and a lane offset past them: such a load asks for nothing and brings zeros.  256 rows are at most
 // kMostExpertPitch values apart, so that every offset that is meant lies below.
 constexpr uint32_t kRecords = 0x80000000u, kNowhere = 0xffffff00u;
 
-// ---- which tile a workgroup takes ---------------------------------------------------------------
-struct Placed {
-    int group, row0, rows, nt;
+// ---- which tiles a workgroup takes --------------------------------------------------------------
+// A tile: where its operands and its result lie.
+struct Work {
+    const char *a, *b;           // the tile's first row, at c = 0
+    int rows_a, rows_b, c;       // rows of the tile that are there, length of the sum
+    int i0, j0;                  // first row and column of the result
+    int group;
 };
-// Row tiles are counted group by group, each with n_tiles column tiles.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of
-// the tiles there are, one after the other.  Every wavefront finds its tile by itself, four groups to a lane; rows = 0
-// where there are fewer tiles than workgroups.
-template <int BM>
-__device__ __forceinline__ Placed place(const GemmArgs &a, int n_tiles)
-{
-    const int lane = threadIdx.x & 63;
-    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
-    auto tile_of = [&](int64_t tiles) {
-        const int64_t total = tiles * n_tiles, share = (total + 7) / 8, id = xcd * share + local;
-        return local < share && id < total ? (int)id : -1;
-    };
-    if (!a.offsets) {
-        const int id = tile_of((a.M + BM - 1) / BM);
-        if (id < 0) return Placed{0, 0, 0, 0};
-        const int row0 = id / n_tiles * BM;
-        return Placed{0, row0, min(BM, a.M - row0), id % n_tiles};
+
+// The items that workgroup b takes one after the other, of `total`: b runs on XCD b % 8, and an XCD takes `block` items in a row of every eight
+// times as many, so that a row tile's rows and a group's matrix are fetched into few L2s while all XCDs get their share of large and small tiles.
+struct Items {
+    int total, block, at, step;
+    __device__ __forceinline__ Items(int64_t n, int workgroups, int most)
+    {
+        const int rounds = (int)((n + workgroups - 1) / workgroups);
+        total = (int)n;
+        block = rounds ? min(most, (int)((n + 8 * rounds - 1) / (8 * rounds))) : 1;
+        at = blockIdx.x >> 3;
+        step = workgroups >> 3;
     }
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.offsets, (uint32_t)(a.groups + 1) * 4);   // entries past the last one come as zeros
+    __device__ __forceinline__ int next()                     // -1: none
+    {
+        const int id = at / block * 8 * block + (blockIdx.x & 7) * block + at % block;
+        at += step;
+        return id < total ? id : -1;
+    }
+};
+
+// Where the groups begin, four of them to a lane.
+struct Groups {
     int at[5];
+    __device__ __forceinline__ explicit Groups(const GemmArgs &g)
+    {
+        const int lane = threadIdx.x & 63;
+        if (!g.offsets) {
 #pragma unroll
-    for (int i = 0; i < 5; ++i) at[i] = max(0, min(a.M, (int)__builtin_amdgcn_raw_buffer_load_b32(r, lane * 16 + i * 4, 0, 0)));
-    int tiles = 0;
+            for (int i = 0; i < 5; ++i) at[i] = i || lane ? g.M : 0;
+        } else {
+            const __amdgpu_buffer_rsrc_t r = make_rsrc(g.offsets, (uint32_t)(g.groups + 1) * 4);   // entries past the last one come as zeros
 #pragma unroll
-    for (int i = 0; i < 4; ++i) tiles += (max(0, at[i + 1] - at[i]) + BM - 1) / BM;
-    int upto = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int v = __shfl_up(upto, d);
-        upto += lane >= d ? v : 0;
-    }
-    const int id = tile_of(__builtin_amdgcn_readlane(upto, 63));
-    if (id < 0) return Placed{0, 0, 0, 0};
-    const int mt = id / n_tiles;
-    const int owner = __builtin_ctzll(__ballot(upto > mt));
-    int left = mt - (upto - tiles), group = 0, row0 = 0, rows = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = (max(0, at[i + 1] - at[i]) + BM - 1) / BM;
-        if (left >= 0 && left < n) {
-            group = lane * 4 + i;
-            row0 = at[i] + left * BM;
-            rows = min(BM, at[i + 1] - row0);
+            for (int i = 0; i < 5; ++i) at[i] = max(0, min(g.M, (int)__builtin_amdgcn_raw_buffer_load_b32(r, lane * 16 + i * 4, 0, 0)));
         }
-        left -= n;
     }
-    return Placed{__builtin_amdgcn_readlane(group, owner), __builtin_amdgcn_readlane(row0, owner), __builtin_amdgcn_readlane(rows, owner), id % n_tiles};
+    // The rows of a group, the same in all lanes.
+    __device__ __forceinline__ void rows(int group, int &from, int &n) const
+    {
+        int begin = 0, end = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            begin = (group & 3) == i ? at[i] : begin;
+            end = (group & 3) == i ? at[i + 1] : end;
+        }
+        from = __builtin_amdgcn_readlane(begin, group >> 2);
+        n = max(0, __builtin_amdgcn_readlane(end, group >> 2) - from);
+    }
+};
+
+// Row tiles are counted group by group; a lane knows how many there are up to its last group.
+template <int BM>
+struct RowTiles : Groups {
+    int upto, total;
+    __device__ __forceinline__ explicit RowTiles(const GemmArgs &g) : Groups(g)
+    {
+        const int lane = threadIdx.x & 63;
+        upto = tiles();
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int v = __shfl_up(upto, d);
+            upto += lane >= d ? v : 0;
+        }
+        total = __builtin_amdgcn_readlane(upto, 63);
+    }
+    __device__ __forceinline__ int tiles_of(int i) const { return (max(0, at[i + 1] - at[i]) + BM - 1) / BM; }
+    __device__ __forceinline__ int tiles() const { return tiles_of(0) + tiles_of(1) + tiles_of(2) + tiles_of(3); }
+    __device__ __forceinline__ void find(int mt, int &group_of, int &row0_of, int &rows_of) const
+    {
+        const int owner = __builtin_ctzll(__ballot(upto > mt));
+        int left = mt - (upto - tiles()), group = 0, row0 = 0, rows = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = tiles_of(i);
+            if (left >= 0 && left < n) {
+                group = (threadIdx.x & 63) * 4 + i;
+                row0 = at[i] + left * BM;
+                rows = min(BM, at[i + 1] - row0);
+            }
+            left -= n;
+        }
+        group_of = __builtin_amdgcn_readlane(group, owner);
+        row0_of = __builtin_amdgcn_readlane(row0, owner);
+        rows_of = __builtin_amdgcn_readlane(rows, owner);
+    }
+};
+
+
+// The groups by their number of rows, the largest first; the lower of equal ones.  Four to a lane, a byte each.
+template <int THREADS>
+__device__ __forceinline__ uint32_t groups_by_rows(const Groups &groups, int n_groups, char *lds)
+{
+    int *rows = reinterpret_cast<int *>(lds);                 // [256]
+    uint8_t *order = reinterpret_cast<uint8_t *>(lds + 1024); // [256]
+    const int tid = threadIdx.x;
+    if (tid < 64) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rows[tid * 4 + i] = max(0, groups.at[i + 1] - groups.at[i]);
+    }
+    __syncthreads();
+    for (int i = tid; i < n_groups; i += THREADS) {
+        const int mine = rows[i];
+        int rank = 0;
+        for (int j = 0; j < n_groups; ++j) {
+            const int n = rows[j];
+            rank += n > mine || (n == mine && j < i) ? 1 : 0;
+        }
+        order[rank] = (uint8_t)i;
+    }
+    __syncthreads();
+    const uint32_t mine = reinterpret_cast<const uint32_t *>(order)[tid & 63];
+    __syncthreads();
+    return mine;
 }
 
 // ---- operand tiles in LDS -----------------------------------------------------------------------
-// 64 values of c at a time, by loads of 1 KiB that go straight into LDS, lane i's 16 bytes to 16 i.
-//   ALONG   c along a row: rows of 128 bytes, piece p of row r at place p ^ (r / 2 & 7), so that neither the loads nor the
-//           reads of one piece of 32 rows meet in a bank
-//   ACROSS  64 rows of c, each with the tile's columns; the 64-byte chunk of 32 columns that a fragment takes is moved
+// KB values of c at a time, by loads of 1 KiB that go straight into LDS, lane i's 16 bytes to 16 i.
+//   ALONG   c along a row: rows of 2 KB bytes, their 16-byte pieces moved by the row, so that neither the loads nor the reads of
+//           one piece of 32 rows meet in a bank
+//   ACROSS  KB rows of c, each with the tile's columns; the 64-byte chunk of 32 columns that a fragment takes is moved
 //           by the row, so that the four rows of a transposing read lie in four quarters of the banks
-template <bool ACROSS, int ROWS>
+template <bool ACROSS, int ROWS, int KB>
 struct Tile {
-    static constexpr int kBytes = ROWS * 128;
-    static constexpr int kPitch = ACROSS ? ROWS * 2 : 128;
+    static constexpr int kBytes = ROWS * KB * 2;
+    static constexpr int kPitch = ACROSS ? ROWS * 2 : KB * 2;
     static constexpr int kLoads = kBytes / 1024;
-    static __device__ __forceinline__ int turn(int r) { return kPitch >= 256 ? r & 3 : kPitch == 128 ? r >> 1 & 1 : 0; }
+    static __device__ __forceinline__ int turn(int r)
+    {
+        if (ACROSS) return kPitch >= 256 ? r & 3 : kPitch == 128 ? r >> 1 & 1 : 0;
+        return KB == 64 ? r >> 1 & 7 : r >> 2 & 3;
+    }
     // Byte offset of a lane's piece of load `w` from the tile's first value, and its c; `rows` of the tile are there.
     static __device__ __forceinline__ void lane_at(int w, int lane, int rows, uint32_t pitch, uint32_t &offset, int &c)
     {
+        const int at = w * 1024 + lane * 16, r = at / kPitch, b = at % kPitch;
         if constexpr (ACROSS) {
-            const int at = w * 1024 + lane * 16, r = at / kPitch, b = at % kPitch;
             const int col = ((b / 64 ^ turn(r)) * 64 + b % 64) / 2;
             c = r;
             offset = col < rows ? (uint32_t)r * pitch + col * 2 : kNowhere;
         } else {
-            const int r = w * 8 + (lane >> 3), piece = (lane & 7) ^ (r >> 1 & 7);
+            const int piece = b / 16 ^ turn(r);
             c = piece * 8;
             offset = r < rows ? (uint32_t)r * pitch + piece * 16 : kNowhere;
         }
     }
-    // Byte offset of a lane's part of the fragment of 32 rows from row 32 m and 16 c from 16 q: lane l has row l % 32, c 8 (l / 32) .. + 7.
+    // A lane's part of the fragment of 32 rows from row 32 m and 16 c from 16 q: lane l has row l % 32, c 8 (l / 32) .. + 7.
     static __device__ __forceinline__ bf16x8 fragment(const char *tile, int lane, int m, int q)
     {
         if constexpr (ACROSS) {
@@ -148,47 +250,47 @@ struct Tile {
             const char *at = tile + (16 * q + r) * kPitch + (m ^ turn(r)) * 64 + (g & 1) * 32 + (lane & 3) * 8;
             typedef __attribute__((address_space(3))) s16x4 lds4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at + 4 * kPitch));   // turn(r + 4) is turn(r)
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at + 4 * kPitch + ((m ^ turn(r + 4)) - (m ^ turn(r))) * 64));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             const int r = lane & 31;
-            return *reinterpret_cast<const bf16x8 *>(tile + (m * 32 + r) * 128 + ((2 * q + (lane >> 5)) ^ (r >> 1 & 7)) * 16);
+            return *reinterpret_cast<const bf16x8 *>(tile + (m * 32 + r) * kPitch + ((2 * q + (lane >> 5)) ^ turn(r)) * 16);
         }
     }
 };
 
 // ---- epilogue -----------------------------------------------------------------------------------
 constexpr float kLog2e = 1.44269504088896340736f, kGelu = 0.79788456080286535588f, kGelu3 = 0.044715f;
-// exp(-u) and 1 / (1 + exp(-u))
-struct Sigmoid {
-    float e, s;
+// Both smooth activations are v sigmoid(u): u = v, or for GELU in its form with tanh twice the tanh's argument.  One way through the code for the two:
+// -u log2 e = v (c0 + c1 v^2), du/dv = d0 + d1 v^2.
+struct Act {
+    int kind;                    // kActNone, kActRelu, or else smooth
+    float c0, c1, d0, d1, most;
+    __device__ __forceinline__ explicit Act(int act)
+    {
+        const bool gelu = act == kActGelu;
+        kind = act;
+        c0 = gelu ? -2 * kGelu * kLog2e : -kLog2e, c1 = gelu ? -2 * kGelu * kGelu3 * kLog2e : 0.f;
+        d0 = gelu ? 2 * kGelu : 1.f, d1 = gelu ? 2 * kGelu * 3 * kGelu3 : 0.f;
+        most = gelu ? 9.f : 80.f;
+    }
+    __device__ __forceinline__ float smooth(float v) const
+    {
+        const float v2 = fminf(v * v, 1e30f);                // 0 times infinity would be NaN
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * (c0 + c1 * v2)));
+        return s == 0.f ? 0.f : v * s;                       // also at -infinity
+    }
+    // s + v s (1 - s) du/dv, with 1 - s = exp(-u) s, which loses nothing where s is close to 1.  Beyond +-80 (SiLU) and +-9 (GELU) the slope is 0 or 1 to
+    // within 2^-80; there the powers of v and exp(-u) would give infinity times 0.
+    __device__ __forceinline__ float smooth_slope(float v) const
+    {
+        v = v > most ? most : v < -most ? -most : v;         // NaN stays
+        const float e = __builtin_amdgcn_exp2f(v * (c0 + c1 * (v * v))), s = __builtin_amdgcn_rcpf(1.f + e);
+        return s + v * (e * s) * s * (d0 + d1 * (v * v));
+    }
 };
-__device__ __forceinline__ Sigmoid sigmoid(float u)
-{
-    const float e = __builtin_amdgcn_exp2f(-u * kLog2e);
-    return Sigmoid{e, __builtin_amdgcn_rcpf(1.f + e)};
-}
-// Both activations are v sigmoid(u): u = v, or for GELU in its form with tanh twice the tanh's argument.
-__device__ __forceinline__ float gelu_u(float v) { return 2 * kGelu * (v + kGelu3 * v * v * v); }
-__device__ __forceinline__ float activated(float v, int act)
-{
-    if (act == kActRelu) return v <= 0.f ? 0.f : v;          // NaN stays
-    if (act == kActNone) return v;
-    const float s = sigmoid(act == kActSilu ? v : gelu_u(v)).s;
-    return s == 0.f ? 0.f : v * s;                           // also at -infinity
-}
-// s + v s (1 - s) du/dv, with 1 - s = exp(-u) s, which loses nothing where s is close to 1.  Beyond +-80 (SiLU) and +-9 (GELU) the slope is 0 or 1 to
-// within 2^-80; there the powers of v and exp(-u) would give infinity times 0.
-__device__ __forceinline__ float slope(float v, int act)
-{
-    if (act == kActNone) return 1.f;
-    if (act == kActRelu) return v > 0.f ? 1.f : v <= 0.f ? 0.f : v;
-    const float most = act == kActSilu ? 80.f : 9.f;
-    v = v > most ? most : v < -most ? -most : v;
-    const Sigmoid g = sigmoid(act == kActSilu ? v : gelu_u(v));
-    const float du = act == kActSilu ? 1.f : 2 * kGelu * (1.f + 3 * kGelu3 * v * v);
-    return g.s + v * (g.e * g.s) * g.s * du;
-}
+__device__ __forceinline__ float relu_of(float v) { return v <= 0.f ? 0.f : v; }                     // NaN stays
+__device__ __forceinline__ float relu_slope(float v) { return v > 0.f ? 1.f : v <= 0.f ? 0.f : v; }  // the same
 
 struct F8 {
     float v[8];
@@ -200,255 +302,332 @@ __device__ __forceinline__ F8 widen(bf16x8 x)
     for (int i = 0; i < 8; ++i) f.v[i] = (float)x[i];
     return f;
 }
-__device__ __forceinline__ F8 read8(const char *base, int64_t at, bool f32)
+// Eight values from `at`, in values; kNone: none (zeros, nothing stored).
+constexpr uint32_t kNone = kNowhere;
+__device__ __forceinline__ F8 read8(__amdgpu_buffer_rsrc_t r, uint32_t at, bool f32)
 {
-    if (!f32) return widen(*reinterpret_cast<const bf16x8 *>(base + at * 2));
-    const f32x4 lo = *reinterpret_cast<const f32x4 *>(base + at * 4), hi = *reinterpret_cast<const f32x4 *>(base + at * 4 + 16);
+    if (!f32) return widen(__builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(at == kNone ? kNowhere : at * 2), 0, 0)));
+    const int from = (int)(at == kNone ? kNowhere : at * 4);
+    const f32x4 lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, from, 0, 0));
+    const f32x4 hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, from, 16, 0));
     return F8{{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
 }
-__device__ __forceinline__ void write8(char *base, int64_t at, bool f32, const F8 &f)
+__device__ __forceinline__ void write8(__amdgpu_buffer_rsrc_t r, uint32_t at, bool f32, const F8 &f)
 {
+    typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
     if (f32) {
-        __builtin_nontemporal_store(f32x4{f.v[0], f.v[1], f.v[2], f.v[3]}, reinterpret_cast<f32x4 *>(base + at * 4));
-        __builtin_nontemporal_store(f32x4{f.v[4], f.v[5], f.v[6], f.v[7]}, reinterpret_cast<f32x4 *>(base + at * 4 + 16));
+        const int to = (int)(at == kNone ? kNowhere : at * 4);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{f.v[0], f.v[1], f.v[2], f.v[3]}), r, to, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{f.v[4], f.v[5], f.v[6], f.v[7]}), r, to, 16, 0);
         return;
     }
     bf16x8 x;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (__bf16)f.v[i];
-    __builtin_nontemporal_store(x, reinterpret_cast<bf16x8 *>(base + at * 2));
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, (int)(at == kNone ? kNowhere : at * 2), 0, 0);
 }
 
-// A workgroup's tile: WI x WJ wavefronts, each MI x NJ blocks of 32 x 32; the sum over c in turns of 64 WC, which WC wavefronts share;
-// S stages of tiles in LDS.
-template <Job JOB, int WI, int WJ, int WC, int MI, int NJ, int S>
+// A workgroup's tile: WI x WJ wavefronts, each MI x NJ blocks of 32 x 32 (rows' blocks dealt in turn, so that a short tile keeps all busy);
+// S stages of KB values of c in LDS.
+template <Job JOB, int WI, int WJ, int MI, int NJ, int S, int KB>
 struct Shape {
     static constexpr bool kAcrossA = JOB == Job::weights, kAcrossB = JOB != Job::product;
-    static constexpr int kWaves = WI * WJ * WC, kThreads = kWaves * 64;
+    static constexpr int kWaves = WI * WJ, kThreads = kWaves * 64;
     static constexpr int BM = 32 * MI * WI, BN = 32 * NJ * WJ;
-    typedef Tile<kAcrossA, BM> A;
-    typedef Tile<kAcrossB, BN> B;
-    static constexpr int kPart = A::kBytes + B::kBytes;                    // 64 values of c
-    static constexpr int kStage = WC * kPart;
-    static constexpr int kLoadsA = WC * A::kLoads / kWaves, kLoadsB = WC * B::kLoads / kWaves;   // of a wavefront and stage
-    static_assert(WC * A::kLoads % kWaves == 0 && WC * B::kLoads % kWaves == 0, "loads are dealt evenly");
-    static constexpr int kTurnPitch = NJ * 128 + 16;
-    static constexpr int kTurn = kWaves * 32 * kTurnPitch;
-    static constexpr int kLds = S * kStage > kTurn ? S * kStage : kTurn;
-    static_assert(WC == 1 || (WI == 1 && WJ == 1 && MI == 1), "parts of a sum");
+    typedef Tile<kAcrossA, BM, KB> A;
+    typedef Tile<kAcrossB, BN, KB> B;
+    static constexpr int kStage = A::kBytes + B::kBytes;
+    static constexpr int kLoadsA = A::kLoads / kWaves, kLoadsB = B::kLoads / kWaves;   // of a wavefront and stage
+    static_assert(A::kLoads % kWaves == 0 && B::kLoads % kWaves == 0, "loads are dealt evenly");
+    static_assert(kWaves % 4 == 0, "a lane has the same piece in all of its loads along c");
+    static constexpr int kBias = JOB == Job::weights ? WJ * 2 * BM * 4 : 0;             // sums of dy's columns
+    static constexpr int kLds = S * kStage + kBias;
+    static constexpr int kPerUnit = kLds <= 80 * 1024 ? 2 : 1;                          // workgroups to a compute unit
 };
 
-// Where the operands and the result of a tile lie.
-struct Work {
-    const char *a, *b;           // the tile's first row, at c = 0
-    uint32_t pitch_a, pitch_b;   // bytes
-    int rows_a, rows_b, c;       // rows of the tile that are there, length of the sum
-    int i0, j0;                  // first row and column of the result
-    int group;
+template <int I>
+struct Int {
+    static constexpr int value = I;
 };
 
-template <class Sh, Job JOB, int WI, int WJ, int WC, int MI, int NJ, int S>
-__device__ __forceinline__ void take_tile(const GemmArgs &g, const Work &w, char *lds)
+// A workgroup walks over its tiles, and treats them as one stream of stages: while one stage is multiplied, the next S are on their way, those of
+// the next tile too, so that neither the results of a tile nor the search for the next one keep loads waiting.  Every tile has S stages at least, so that
+// the stream is never more than one tile ahead.
+template <Job JOB, int WI, int WJ, int MI, int NJ, int S, int KB>
+__global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, S, KB>::kWaves * Shape<JOB, WI, WJ, MI, NJ, S, KB>::kPerUnit / 4)) void expert_gemm_tiles(const GemmArgs g)
 {
+    typedef Shape<JOB, WI, WJ, MI, NJ, S, KB> Sh;
     typedef typename Sh::A A;
     typedef typename Sh::B B;
-    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wc = wave % WC, wj = wave / WC % WJ, wi = wave / (WC * WJ);
+    const int wj = wave % WJ, wi = wave / WJ;
+    const int cols = JOB == Job::product ? g.N : g.K, col_tiles = (cols + Sh::BN - 1) / Sh::BN;
+    const uint32_t pitch_a = (uint32_t)g.lda * 2, pitch_b = (uint32_t)g.ldb * 2;
 
+    // ---- the tiles
+    const std::conditional_t<JOB == Job::weights, Groups, RowTiles<Sh::BM>> rows(g);
+    const int tiles_i = JOB == Job::weights ? (g.N + Sh::BM - 1) / Sh::BM : 0;
+    uint32_t order = 0;
+    if constexpr (JOB == Job::weights) order = groups_by_rows<Sh::kThreads>(rows, g.groups, lds);
+    int64_t total;
+    if constexpr (JOB == Job::weights) total = (int64_t)g.groups * tiles_i * col_tiles;
+    else total = (int64_t)rows.total * col_tiles;
+    Items items(total, gridDim.x, 64);
+    auto next = [&](Work &w) {
+        const int id = items.next();
+        if (id < 0) return false;
+        if constexpr (JOB == Job::weights) {
+            const int at = id / (tiles_i * col_tiles), tile = id % (tiles_i * col_tiles);
+            w.group = __builtin_amdgcn_readlane(order, at >> 2) >> (at & 3) * 8 & 255;
+            int from;
+            rows.rows(w.group, from, w.c);
+            w.i0 = tile / col_tiles * Sh::BM, w.j0 = tile % col_tiles * Sh::BN;
+            w.a = g.a + ((int64_t)from * g.lda + w.i0) * 2, w.b = g.b + ((int64_t)from * g.ldb + w.j0) * 2;
+            w.rows_a = min(Sh::BM, g.N - w.i0);
+        } else {
+            rows.find(id / col_tiles, w.group, w.i0, w.rows_a);
+            w.j0 = id % col_tiles * Sh::BN;
+            w.a = g.a + (int64_t)w.i0 * g.lda * 2;
+            w.b = g.b + (w.group * g.b_group + (JOB == Job::product ? w.j0 * g.ldb : (int64_t)w.j0)) * 2;
+            w.c = JOB == Job::product ? g.K : g.N;
+        }
+        w.rows_b = min(Sh::BN, cols - w.j0);
+        w = Work{uniform(w.a), uniform(w.b), uniform(w.rows_a), uniform(w.rows_b), uniform(w.c), uniform(w.i0), uniform(w.j0), uniform(w.group)};
+        return true;
+    };
+    auto stages_of = [&](const Work &w) { return max(S, (w.c + KB - 1) / KB); };
+
+    const uint32_t lds_at = (uint32_t)uniform((int)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
+
+    // ---- loads.  A lane's offsets from where a stage begins in memory, and, for an operand along c, the lane's first value of c, by which a stage
+    // that is not whole leaves loads out.  Across c the descriptor ends with the last row.
     uint32_t off_a[Sh::kLoadsA], off_b[Sh::kLoadsB];
-    int c_a[Sh::kLoadsA], c_b[Sh::kLoadsB];
-#pragma unroll
-    for (int i = 0; i < Sh::kLoadsA; ++i) {
-        const int at = i * Sh::kWaves + wave;
-        A::lane_at(at % A::kLoads, lane, w.rows_a, w.pitch_a, off_a[i], c_a[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < Sh::kLoadsB; ++i) {
-        const int at = i * Sh::kWaves + wave;
-        B::lane_at(at % B::kLoads, lane, w.rows_b, w.pitch_b, off_b[i], c_b[i]);
-    }
-    const int64_t step_a = Sh::kAcrossA ? (int64_t)64 * w.pitch_a : 128, step_b = Sh::kAcrossB ? (int64_t)64 * w.pitch_b : 128;
-    const int stages = (w.c + 64 * WC - 1) / (64 * WC);
-    auto load = [&](int stage, int slot) {
-        char *dst = lds + slot * Sh::kStage;
-#pragma unroll
-        for (int i = 0; i < Sh::kLoadsA; ++i) {
-            const int at = i * Sh::kWaves + wave, part = at / A::kLoads, step = stage * WC + part, c0 = step * 64;
-            const bool in = c0 < w.c;                         // a step past the end asks for nothing
-            const __amdgpu_buffer_rsrc_t r = make_rsrc(w.a + (in ? step * step_a : 0), kRecords);
-            load_to_lds(r, in && c0 + c_a[i] < w.c ? off_a[i] : kNowhere, dst + part * Sh::kPart + at % A::kLoads * 1024);
+    int c_a, c_b;
+    Work ahead;                                               // the tile that is loaded
+    bool more;
+    const char *from_a = nullptr, *from_b = nullptr;          // its next stage, of which `left` values of c are there
+    int left = 0, to_load = 0, to_slot = 0;                   // stages of it still to be asked for
+    auto begin = [&] {
+        more = next(ahead);
+        if (!more) {
+            left = 0, to_load = INT32_MAX;
+            return;
         }
+        const int l = anew(lane);
 #pragma unroll
-        for (int i = 0; i < Sh::kLoadsB; ++i) {
-            const int at = i * Sh::kWaves + wave, part = at / B::kLoads, step = stage * WC + part, c0 = step * 64;
-            const bool in = c0 < w.c;
-            const __amdgpu_buffer_rsrc_t r = make_rsrc(w.b + (in ? step * step_b : 0), kRecords);
-            load_to_lds(r, in && c0 + c_b[i] < w.c ? off_b[i] : kNowhere, dst + part * Sh::kPart + A::kBytes + at % B::kLoads * 1024);
-        }
+        for (int i = 0; i < Sh::kLoadsA; ++i) A::lane_at(i * Sh::kWaves + wave, l, ahead.rows_a, pitch_a, off_a[i], c_a);
+#pragma unroll
+        for (int i = 0; i < Sh::kLoadsB; ++i) B::lane_at(i * Sh::kWaves + wave, l, ahead.rows_b, pitch_b, off_b[i], c_b);
+        from_a = ahead.a, from_b = ahead.b, left = ahead.c, to_load = stages_of(ahead);
+    };
+    auto load = [&] {                                         // behind the last tile it asks for nothing
+        if (to_load == 0) begin();
+        const int there = max(left, 0);
+        const uint32_t dst = lds_at + to_slot * Sh::kStage + wave * 1024;
+        const i32x4 ra = lds_source(from_a, (uint32_t)uniform((int)(Sh::kAcrossA ? (uint32_t)min(there, KB) * pitch_a : there ? kRecords : 0)));
+        const i32x4 rb = lds_source(from_b, (uint32_t)uniform((int)(Sh::kAcrossB ? (uint32_t)min(there, KB) * pitch_b : there ? kRecords : 0)));
+#pragma unroll
+        for (int i = 0; i < Sh::kLoadsA; ++i)
+            load_to_lds(ra, Sh::kAcrossA || c_a < there ? off_a[i] : kNowhere, dst + i * Sh::kWaves * 1024);
+#pragma unroll
+        for (int i = 0; i < Sh::kLoadsB; ++i)
+            load_to_lds(rb, Sh::kAcrossB || c_b < there ? off_b[i] : kNowhere, dst + A::kBytes + i * Sh::kWaves * 1024);
+        left -= min(left, KB);
+        from_a += left > 0 ? (Sh::kAcrossA ? (int64_t)KB * pitch_a : KB * 2) : 0;
+        from_b += left > 0 ? (Sh::kAcrossB ? (int64_t)KB * pitch_b : KB * 2) : 0;
+        --to_load;
+        to_slot = to_slot == S - 1 ? 0 : to_slot + 1;
     };
 
-    f32x16 acc[MI][NJ];
+    begin();
+    if (!more) return;
 #pragma unroll
-    for (int m = 0; m < MI; ++m)
+    for (int s = 0; s < S; ++s) load();
+    wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    int slot = 0;
+
+    // A tile of which this wavefront has `blocks` blocks of rows.
+    auto take = [&](const Work &w, auto blocks) {
+        constexpr int MB = decltype(blocks)::value, MR = MB ? MB : 1, Q = KB / 16;
+        const int stages = stages_of(w);
+        f32x16 acc[MR][NJ];
 #pragma unroll
-        for (int n = 0; n < NJ; ++n)
+        for (int m = 0; m < MB; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[m][n][r] = 0;
-    float bias_part[MI] = {};                                 // weights: sums of dy's columns, this wavefront's share of c
-    const bool sum_bias = JOB == Job::weights && g.d_bias && w.j0 == 0;
-    auto multiply = [&](int slot) {
-        const char *ta = lds + slot * Sh::kStage + wc * Sh::kPart, *tb = ta + A::kBytes;
+            for (int n = 0; n < NJ; ++n)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            bf16x8 fa[MI], fb[NJ];
+                for (int r = 0; r < 16; ++r) acc[m][n][r] = 0;
+        float bias_part[MR] = {};                             // weights: sums of dy's columns, this wavefront's share of c
+        int sum_bias = JOB == Job::weights && g.d_bias && w.j0 == 0;
+
+        // Fragments of 16 values of c are read one step of products ahead, the first ones of a stage behind the barrier that says that the stage is
+        // there; that stands in front of the last products of the stage before, so that nobody waits for LDS with idle matrix cores.
+        bf16x8 fa[2][MR], fb[2][NJ];
+        auto fetch = [&](int q, int to) {
+            if constexpr (MB > 0) {
+                const char *ta = lds + slot * Sh::kStage, *tb = ta + A::kBytes;
 #pragma unroll
-            for (int m = 0; m < MI; ++m) fa[m] = A::fragment(ta, lane, m * WI + wi, q);
+                for (int n = 0; n < NJ; ++n) fb[to][n] = B::fragment(tb, lane, wj * NJ + n, q);
 #pragma unroll
-            for (int n = 0; n < NJ; ++n) fb[n] = B::fragment(tb, lane, n * WJ + wj, q);
+                for (int m = 0; m < MB; ++m) fa[to][m] = A::fragment(ta, lane, m * WI + wi, q);
+            }
+        };
+        auto products = [&](int t, int q) {
+            const int of = q & 1;
 #pragma unroll
-            for (int m = 0; m < MI; ++m)
+            for (int m = 0; m < MB; ++m)
 #pragma unroll
-                for (int n = 0; n < NJ; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[n], fa[m], acc[m][n], 0, 0, 0);
-            if (JOB == Job::weights && sum_bias && q % WJ == wj) {
+                for (int n = 0; n < NJ; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[of][n], fa[of][m], acc[m][n], 0, 0, 0);
+            if (JOB == Job::weights) sum_bias = hidden(sum_bias);
+            if (JOB == Job::weights && sum_bias && (t * Q + q) % WJ == wj) {
 #pragma unroll
-                for (int m = 0; m < MI; ++m) {
-                    const F8 f = widen(fa[m]);
+                for (int m = 0; m < MB; ++m) {
+                    const F8 f = widen(fa[of][m]);
                     bias_part[m] += ((f.v[0] + f.v[1]) + (f.v[2] + f.v[3])) + ((f.v[4] + f.v[5]) + (f.v[6] + f.v[7]));
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // The next stage is there, and nobody reads this one any more.  The first S stages of a tile are there when it begins: they are waited for in front of
+        // the stores of the tile before, so that no wait for them is one for stores.
+        int there = S - 1;                                    // stages that are, besides the one that is multiplied
+        auto arrived = [&] {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            there = hidden(there - 1);
+            if (there < 0) wait_loads<(S - 2) * (Sh::kLoadsA + Sh::kLoadsB)>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        fetch(0, 0);
+#pragma clang loop unroll(disable)
+        for (int t = 0; t < stages; ++t) {
+#pragma unroll
+            for (int q = 0; q < Q - 1; ++q) {
+                fetch(q + 1, q + 1 & 1);
+                products(t, q);
+            }
+            slot = slot == S - 1 ? 0 : slot + 1;
+            arrived();
+            load();
+            if (t + 1 < stages) fetch(0, 0);                  // the next tile's first are read when it begins
+            products(t, Q - 1);
+        }
+
+        // ---- results.  A lane holds four times four consecutive columns of one row of a block, and lane ^ 32 the four beside them; exchanged, it holds twice eight.
+        const Act act(g.activation);
+        const int size = g.out32 ? 4 : 2;
+        // What a call has beside the result; the compiler is kept from making a copy of all this for each of the possibilities.
+        int has_bias = g.bias != nullptr, has_pre = g.pre != nullptr, has_residual = g.residual != nullptr, out32 = g.out32, kind = act.kind;
+        const __amdgpu_buffer_rsrc_t ro = make_rsrc(g.out + ((JOB == Job::weights ? w.group * g.out_group : 0) + (int64_t)w.i0 * g.ldo + w.j0) * size, kRecords);
+        const __amdgpu_buffer_rsrc_t rp = make_rsrc(g.pre + ((int64_t)w.i0 * g.ld_pre + w.j0) * 2, kRecords);
+        const __amdgpu_buffer_rsrc_t rr = make_rsrc(g.residual + ((int64_t)w.i0 * g.ld_res + w.j0) * size, kRecords);
+        const __amdgpu_buffer_rsrc_t rb = make_rsrc(g.bias + (JOB == Job::product ? (int64_t)w.group * g.N + w.j0 : 0), kRecords);
+        wait_loads<0>();
+        const int l = anew(lane);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+            const int i = (m * WI + wi) * 32 + (l & 31);
+#pragma unroll
+            for (int n = 0; n < NJ; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int j = (wj * NJ + n) * 32 + h * 16 + (l >> 5) * 8;
+                    const bool in = i < w.rows_a && j < w.rows_b;
+                    has_bias = hidden(has_bias), has_pre = hidden(has_pre), has_residual = hidden(has_residual), out32 = hidden(out32), kind = hidden(kind);
+                    F8 f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float lo = acc[m][n][h * 8 + e], hi = acc[m][n][h * 8 + 4 + e];
+                        const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi), false, false);
+                        const uint32_t first = both[0], second = both[1];
+                        f.v[e] = __builtin_bit_cast(float, first);
+                        f.v[4 + e] = __builtin_bit_cast(float, second);
+                    }
+                    if constexpr (JOB == Job::product) {
+                        if (has_bias) {
+                            const F8 b = read8(rb, j < w.rows_b ? (uint32_t)j : kNone, true);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f.v[e] += b.v[e];
+                        }
+                        if (has_pre) write8(rp, in ? i * (uint32_t)g.ld_pre + j : kNone, false, f);
+                        if (kind >= kActGelu) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f.v[e] = act.smooth(f.v[e]);
+                        } else if (kind == kActRelu) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f.v[e] = relu_of(f.v[e]);
+                        }
+                        if (has_residual) {
+                            const F8 s = read8(rr, in ? i * (uint32_t)g.ld_res + j : kNone, out32);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f.v[e] += s.v[e];
+                        }
+                    } else if constexpr (JOB == Job::input) {
+                        if (has_pre) {
+                            const F8 s = read8(rp, in ? i * (uint32_t)g.ld_pre + j : kNone, false);
+                            if (kind >= kActGelu) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) f.v[e] *= act.smooth_slope(s.v[e]);
+                            } else if (kind == kActRelu) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) f.v[e] *= relu_slope(s.v[e]);
+                            }
+                        }
+                    }
+                    write8(ro, in ? i * (uint32_t)g.ldo + j : kNone, out32, f);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+        if (JOB == Job::weights && sum_bias) {                // the wavefronts' shares of a column, in a fixed order
+            float *part = reinterpret_cast<float *>(lds + S * Sh::kStage);   // [WJ][2][BM]
+#pragma unroll
+            for (int m = 0; m < MB; ++m) part[(wj * 2 + (l >> 5)) * Sh::BM + (m * WI + wi) * 32 + (l & 31)] = bias_part[m];
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            for (int i = tid; i < w.rows_a; i += Sh::kThreads) {
+                float sum = 0;
+                for (int p = 0; p < 2 * WJ; ++p) sum += part[p * Sh::BM + i];
+                g.d_bias[(int64_t)w.group * g.N + w.i0 + i] = sum;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-#pragma unroll
-    for (int s = 0; s < S - 1; ++s) load(s, s);
-    int slot = 0;
-    for (int t = 0; t < stages; ++t) {
-        wait_loads<(S - 2) * (Sh::kLoadsA + Sh::kLoadsB)>();
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        load(t + S - 1, slot ? slot - 1 : S - 1);
-        multiply(slot);
-        slot = slot == S - 1 ? 0 : slot + 1;
-    }
-    wait_loads<0>();                                          // the last loads still write LDS
-    __syncthreads();
-
-    // A lane holds four times four columns of one row of a block; through LDS, in fp32, to eight consecutive columns of a row, so that
-    // what is read and written beside the result goes by whole lines.  Parts of a sum are added here, in a fixed order.
-    const bool out32 = g.out32;
-#pragma unroll
-    for (int m = 0; m < MI; ++m) {
-        char *turn = lds + wave * 32 * Sh::kTurnPitch;
-#pragma unroll
-        for (int n = 0; n < NJ; ++n)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<f32x4 *>(turn + (lane & 31) * Sh::kTurnPitch + (n * 32 + q * 8 + half * 4) * 4) =
-                    f32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
-        if (WC > 1) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
-        constexpr int kPieces = 32 * NJ * 4, kTakers = 64 * WC;
-        for (int p = WC > 1 ? tid : lane; p < kPieces; p += kTakers) {
-            const int r = p / (NJ * 4), c8 = p % (NJ * 4);
-            const int i = w.i0 + (m * WI + wi) * 32 + r, jn = c8 / 4, j = w.j0 + (jn * WJ + wj) * 32 + c8 % 4 * 8;
-            if (i - w.i0 >= w.rows_a || j - w.j0 >= w.rows_b) continue;
-            const char *src = WC > 1 ? lds : turn;
-            F8 f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f.v[e] = 0;
-#pragma unroll
-            for (int part = 0; part < WC; ++part) {
-                const f32x4 *at = reinterpret_cast<const f32x4 *>(src + (part * 32 + r) * Sh::kTurnPitch + c8 * 32);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f.v[e] += at[0][e], f.v[4 + e] += at[1][e];
-            }
-            if constexpr (JOB == Job::product) {
-                if (g.bias) {
-                    const F8 b = read8((const char *)g.bias, (int64_t)w.group * g.N + j, true);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f.v[e] += b.v[e];
-                }
-                if (g.pre) write8(g.pre, (int64_t)i * g.ld_pre + j, false, f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f.v[e] = activated(f.v[e], g.activation);
-                if (g.residual) {
-                    const F8 s = read8(g.residual, (int64_t)i * g.ld_res + j, out32);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f.v[e] += s.v[e];
-                }
-                write8(g.out, (int64_t)i * g.ldo + j, out32, f);
-            } else if constexpr (JOB == Job::input) {
-                if (g.pre) {
-                    const F8 s = read8(g.pre, (int64_t)i * g.ld_pre + j, false);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f.v[e] *= slope(s.v[e], g.activation);
-                }
-                write8(g.out, (int64_t)i * g.ldo + j, out32, f);
-            } else {
-                write8(g.out, w.group * g.out_group + (int64_t)i * g.ldo + j, out32, f);
-            }
-        }
-        if (WC > 1) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
-    }
-    if (JOB == Job::weights && sum_bias) {                    // the wavefronts' shares of a column, in a fixed order
-        __syncthreads();
-        float *part = reinterpret_cast<float *>(lds);         // [WJ][2][BM]
-#pragma unroll
-        for (int m = 0; m < MI; ++m) part[(wj * 2 + half) * Sh::BM + (m * WI + wi) * 32 + (lane & 31)] = bias_part[m];
-        __syncthreads();
-        for (int i = tid; i < Sh::BM; i += Sh::kThreads) {
-            if (i >= w.rows_a) continue;
-            float sum = 0;
-            for (int p = 0; p < 2 * WJ; ++p) sum += part[p * Sh::BM + i];
-            g.d_bias[(int64_t)w.group * g.N + w.i0 + i] = sum;
-        }
+    while (true) {
+        const Work w = ahead;
+        const int blocks = ((w.rows_a + 31) / 32 - wi + WI - 1) / WI;
+        if (blocks <= 0) take(w, Int<0>());
+        else if (MI == 1 || blocks == 1) take(w, Int<1>());
+        else if (MI == 2 || blocks == 2) take(w, Int<(MI < 2 ? MI : 2)>());
+        else if (MI == 3 || blocks == 3) take(w, Int<(MI < 3 ? MI : 3)>());
+        else take(w, Int<MI>());
+        if (!more) break;
     }
 }
 
-template <Job JOB, int WI, int WJ, int WC, int MI, int NJ, int S>
-__global__ __launch_bounds__(WI *WJ *WC * 64) void expert_gemm_tiles(const GemmArgs g)
-{
-    typedef Shape<JOB, WI, WJ, WC, MI, NJ, S> Sh;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    Work w;
-    if constexpr (JOB == Job::weights) {
-        const int ti = (g.N + Sh::BM - 1) / Sh::BM, tj = (g.K + Sh::BN - 1) / Sh::BN;
-        const int tile = blockIdx.x % (ti * tj), group = blockIdx.x / (ti * tj);
-        const int from = g.offsets ? max(0, min(g.M, g.offsets[group])) : 0, to = g.offsets ? max(0, min(g.M, g.offsets[group + 1])) : g.M;
-        w.group = group, w.i0 = tile / tj * Sh::BM, w.j0 = tile % tj * Sh::BN;
-        w.a = g.a + ((int64_t)from * g.lda + w.i0) * 2, w.b = g.b + ((int64_t)from * g.ldb + w.j0) * 2;
-        w.rows_a = min(Sh::BM, g.N - w.i0), w.rows_b = min(Sh::BN, g.K - w.j0), w.c = max(0, to - from);
-    } else {
-        const int cols = JOB == Job::product ? g.N : g.K;
-        const Placed at = place<Sh::BM>(g, (cols + Sh::BN - 1) / Sh::BN);
-        if (at.rows == 0) return;
-        w.group = at.group, w.i0 = at.row0, w.j0 = at.nt * Sh::BN;
-        w.a = g.a + (int64_t)at.row0 * g.lda * 2;
-        w.b = g.b + (at.group * g.b_group + (JOB == Job::product ? w.j0 * g.ldb : (int64_t)w.j0)) * 2;
-        w.rows_a = at.rows, w.rows_b = min(Sh::BN, cols - w.j0), w.c = JOB == Job::product ? g.K : g.N;
-    }
-    w.pitch_a = (uint32_t)g.lda * 2, w.pitch_b = (uint32_t)g.ldb * 2;
-    take_tile<Sh, JOB, WI, WJ, WC, MI, NJ, S>(g, w, lds);
-}
-
-template <Job JOB, int WI, int WJ, int WC, int MI, int NJ, int S>
+template <Job JOB, int WI, int WJ, int MI, int NJ, int S, int KB>
 int launch_shape(const GemmArgs &g, hipStream_t st)
 {
-    typedef Shape<JOB, WI, WJ, WC, MI, NJ, S> Sh;
+    typedef Shape<JOB, WI, WJ, MI, NJ, S, KB> Sh;
     static LdsGrant grant;
-    const void *kernel = (const void *)expert_gemm_tiles<JOB, WI, WJ, WC, MI, NJ, S>;
+    const void *kernel = (const void *)expert_gemm_tiles<JOB, WI, WJ, MI, NJ, S, KB>;
     const int e = allow_lds(grant, kernel, Sh::kLds);
     if (e) return e;
-    int64_t grid;
+    int64_t tiles;                                            // at most
     if (JOB == Job::weights) {
-        grid = (int64_t)g.groups * ((g.N + Sh::BM - 1) / Sh::BM) * ((g.K + Sh::BN - 1) / Sh::BN);
+        tiles = (int64_t)g.groups * ((g.N + Sh::BM - 1) / Sh::BM) * ((g.K + Sh::BN - 1) / Sh::BN);
     } else {
         const int cols = JOB == Job::product ? g.N : g.K;
-        const int64_t tiles = g.M / Sh::BM + (g.groups < g.M ? g.groups : g.M);
-        grid = (tiles * ((cols + Sh::BN - 1) / Sh::BN) + 7) / 8 * 8;
+        tiles = (int64_t)(g.M / Sh::BM + (g.groups < g.M ? g.groups : g.M)) * ((cols + Sh::BN - 1) / Sh::BN);
     }
-    expert_gemm_tiles<JOB, WI, WJ, WC, MI, NJ, S><<<(uint32_t)grid, Sh::kThreads, Sh::kLds, st>>>(g);
+    const int64_t most = Sh::kPerUnit * stream_compute_units(st), grid = tiles < most ? (tiles + 7) / 8 * 8 : most;
+    expert_gemm_tiles<JOB, WI, WJ, MI, NJ, S, KB><<<(uint32_t)grid, Sh::kThreads, Sh::kLds, st>>>(g);
     return (int)hipGetLastError();
 }
 
@@ -468,7 +647,7 @@ int launch_expert_gemm(const ExpertGemmShape &s, const void *x, int64_t ldx, int
     g.a = (const char *)x, g.lda = ldx, g.b = (const char *)w, g.ldb = s.K, g.b_group = (int64_t)s.N * s.K;
     g.bias = bias, g.pre = (char *)pre, g.ld_pre = ld_pre, g.residual = (const char *)residual, g.ld_res = ld_res;
     g.out = (char *)y, g.ldo = ldy;
-    return launch_shape<Job::product, 2, 2, 1, 2, 2, 2>(g, st);
+    return launch_shape<Job::product, 2, 4, 4, 2, 2, 64>(g, st);
 }
 
 int launch_expert_gemm_input(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, int32_t M, const void *w, const int32_t *offsets, const void *pre,
@@ -478,7 +657,7 @@ int launch_expert_gemm_input(const ExpertGemmShape &s, const void *dy, int64_t l
     g.a = (const char *)dy, g.lda = ld_dy, g.b = (const char *)w, g.ldb = s.K, g.b_group = (int64_t)s.N * s.K;
     g.pre = (char *)const_cast<void *>(pre), g.ld_pre = ld_pre;
     g.out = (char *)dx, g.ldo = ld_dx;
-    return launch_shape<Job::input, 2, 2, 1, 2, 2, 2>(g, st);
+    return launch_shape<Job::input, 2, 4, 4, 2, 2, 64>(g, st);
 }
 
 int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, int32_t M, const int32_t *offsets,
@@ -487,7 +666,7 @@ int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t
     GemmArgs g = args_of(s, offsets, M);
     g.a = (const char *)dy, g.lda = ld_dy, g.b = (const char *)x, g.ldb = ldx;
     g.out = (char *)dw, g.ldo = s.K, g.out_group = (int64_t)s.N * s.K, g.d_bias = d_bias;
-    return launch_shape<Job::weights, 2, 2, 1, 2, 2, 2>(g, st);
+    return launch_shape<Job::weights, 2, 4, 4, 2, 2, 64>(g, st);
 }
 
 }  // namespace sida
