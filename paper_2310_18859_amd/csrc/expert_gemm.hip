@@ -49,15 +49,16 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, ui
 }
 // 16 bytes a lane straight into LDS: lane i's land at dst + 16 i.  Written out, because the compiler waits for all that it knows to be on its way to LDS
 // in front of each transposing read (8192 cubed, the input's gradient: 1089 us against 947); it has no register as its result, and waits that the compiler
-// counts without it wait longer, never shorter.  The pauses: a scalar register written by a vector instruction, or M0, is not there at once.
+// counts without it wait longer, never shorter.  The pause: M0 is not there at once; settle() is that for scalar registers written by vector instructions.
 __device__ __forceinline__ i32x4 lds_source(const char *base, uint32_t bytes)
 {
     return i32x4{(int)(uint32_t)(uint64_t)base, (int)((uint64_t)base >> 32 & 0xffff), (int)bytes, 0x00020000};
 }
 __device__ __forceinline__ void load_to_lds(i32x4 source, uint32_t offset, uint32_t dst)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(offset), "s"(source) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(offset), "s"(source) : "memory");
 }
+__device__ __forceinline__ void settle(i32x4 &a, i32x4 &b) { asm volatile("s_nop 4" : "+s"(a), "+s"(b)); }
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
@@ -328,21 +329,56 @@ __device__ __forceinline__ void write8(__amdgpu_buffer_rsrc_t r, uint32_t at, bo
 }
 
 // A workgroup's tile: WI x WJ wavefronts, each MI x NJ blocks of 32 x 32 (rows' blocks dealt in turn, so that a short tile keeps all busy);
-// S stages of KB values of c in LDS.
-template <Job JOB, int WI, int WJ, int MI, int NJ, int S, int KB>
+// SA and SB stages of KB values of c of the two operands in LDS.
+template <Job JOB, int WI, int WJ, int MI, int NJ, int SA, int SB, int KB>
 struct Shape {
     static constexpr bool kAcrossA = JOB == Job::weights, kAcrossB = JOB != Job::product;
     static constexpr int kWaves = WI * WJ, kThreads = kWaves * 64;
     static constexpr int BM = 32 * MI * WI, BN = 32 * NJ * WJ;
     typedef Tile<kAcrossA, BM, KB> A;
     typedef Tile<kAcrossB, BN, KB> B;
-    static constexpr int kStage = A::kBytes + B::kBytes;
-    static constexpr int kLoadsA = A::kLoads / kWaves, kLoadsB = B::kLoads / kWaves;   // of a wavefront and stage
     static_assert(A::kLoads % kWaves == 0 && B::kLoads % kWaves == 0, "loads are dealt evenly");
     static_assert(kWaves % 4 == 0, "a lane has the same piece in all of its loads along c");
-    static constexpr int kBias = JOB == Job::weights ? WJ * 2 * BM * 4 : 0;             // sums of dy's columns
-    static constexpr int kLds = S * kStage + kBias;
+    static constexpr int kLoadsA = A::kLoads / kWaves, kLoadsB = B::kLoads / kWaves;   // of a wavefront and stage
+    // The operand that is further ahead, by one stage, is asked for behind the other, so that waiting for that leaves it out.
+    static constexpr bool kLeadB = SB > SA;
+    static constexpr int S = SA < SB ? SA : SB, kMost = SA > SB ? SA : SB;
+    static_assert(S >= 2 && kMost - S <= 1, "stages");
+    static constexpr int kLater = (S - 2) * (kLoadsA + kLoadsB) + (SA > SB ? kLoadsA : SB > SA ? kLoadsB : 0);   // loads behind the ones waited for
+    static constexpr int kLds = SA * A::kBytes + SB * B::kBytes;
     static constexpr int kPerUnit = kLds <= 80 * 1024 ? 2 : 1;                          // workgroups to a compute unit
+};
+
+// One operand's loads: a ring of S stages in LDS, and where the next stage comes from.  A lane's offsets are from where a stage begins in memory; along c its
+// first value of c says which loads a stage that is not whole leaves out, across c the descriptor ends with the last row.
+template <class T, bool ACROSS, int S, int KB, int WAVES>
+struct Ring {
+    static constexpr int kLoads = T::kLoads / WAVES;
+    uint32_t off[kLoads], lds_at, pitch;
+    int c;
+    const char *from = nullptr;
+    int left = 0, to_load = 0, slot = 0;                      // values of c, and stages, of the tile that are still to be asked for
+    i32x4 source;
+    uint32_t dst, there;
+    __device__ __forceinline__ Ring(uint32_t lds, uint32_t pitch_, int wave) : lds_at(lds + wave * 1024), pitch(pitch_) {}
+    __device__ __forceinline__ void begin(const char *tile, int rows, int length, int stages, int lane, int wave)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) T::lane_at(i * WAVES + wave, lane, rows, pitch, off[i], c);
+        from = tile, left = length, to_load = stages;
+    }
+    __device__ __forceinline__ void end() { left = 0, to_load = INT32_MAX; }              // asks for nothing from now on
+    __device__ __forceinline__ void prepare()
+    {
+        there = left;
+        source = lds_source(from, (uint32_t)uniform((int)(ACROSS ? (uint32_t)min(left, KB) * pitch : left ? kRecords : 0)));
+        dst = lds_at + slot * T::kBytes;
+        left -= min(left, KB);
+        from += left > 0 ? (ACROSS ? (int64_t)KB * pitch : KB * 2) : 0;
+        --to_load;
+        slot = slot == S - 1 ? 0 : slot + 1;
+    }
+    __device__ __forceinline__ void load(int i) { load_to_lds(source, ACROSS || c < (int)there ? off[i] : kNowhere, dst + i * WAVES * 1024); }
 };
 
 template <int I>
@@ -350,21 +386,21 @@ struct Int {
     static constexpr int value = I;
 };
 
-// A workgroup walks over its tiles, and treats them as one stream of stages: while one stage is multiplied, the next S are on their way, those of
-// the next tile too, so that neither the results of a tile nor the search for the next one keep loads waiting.  Every tile has S stages at least, so that
-// the stream is never more than one tile ahead.
-template <Job JOB, int WI, int WJ, int MI, int NJ, int S, int KB>
-__global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, S, KB>::kWaves * Shape<JOB, WI, WJ, MI, NJ, S, KB>::kPerUnit / 4)) void expert_gemm_tiles(const GemmArgs g)
+// A workgroup walks over its tiles, and treats them as one stream of stages: while one stage is multiplied, the next ones are on their way, those of
+// the next tile too, so that neither the results of a tile nor the search for the next one keep loads waiting.  Every tile has as many stages as there are
+// in LDS at least, so that the stream is never more than one tile ahead.
+template <Job JOB, int WI, int WJ, int MI, int NJ, int SA, int SB, int KB>
+__global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB>::kWaves * Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB>::kPerUnit / 4)) void expert_gemm_tiles(const GemmArgs g)
 {
-    typedef Shape<JOB, WI, WJ, MI, NJ, S, KB> Sh;
+    typedef Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB> Sh;
     typedef typename Sh::A A;
     typedef typename Sh::B B;
+    constexpr int S = Sh::S;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wj = wave % WJ, wi = wave / WJ;
     const int cols = JOB == Job::product ? g.N : g.K, col_tiles = (cols + Sh::BN - 1) / Sh::BN;
-    const uint32_t pitch_a = (uint32_t)g.lda * 2, pitch_b = (uint32_t)g.ldb * 2;
 
     // ---- the tiles
     const std::conditional_t<JOB == Job::weights, Groups, RowTiles<Sh::BM>> rows(g);
@@ -397,61 +433,79 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, S, KB>::kW
         w = Work{uniform(w.a), uniform(w.b), uniform(w.rows_a), uniform(w.rows_b), uniform(w.c), uniform(w.i0), uniform(w.j0), uniform(w.group)};
         return true;
     };
-    auto stages_of = [&](const Work &w) { return max(S, (w.c + KB - 1) / KB); };
+    auto stages_of = [&](const Work &w) { return max(Sh::kMost, (w.c + KB - 1) / KB); };
 
+    // ---- loads
     const uint32_t lds_at = (uint32_t)uniform((int)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
-
-    // ---- loads.  A lane's offsets from where a stage begins in memory, and, for an operand along c, the lane's first value of c, by which a stage
-    // that is not whole leaves loads out.  Across c the descriptor ends with the last row.
-    uint32_t off_a[Sh::kLoadsA], off_b[Sh::kLoadsB];
-    int c_a, c_b;
+    Ring<A, Sh::kAcrossA, SA, KB, Sh::kWaves> ra(lds_at, (uint32_t)g.lda * 2, wave);
+    Ring<B, Sh::kAcrossB, SB, KB, Sh::kWaves> rb(lds_at + SA * A::kBytes, (uint32_t)g.ldb * 2, wave);
     Work ahead;                                               // the tile that is loaded
-    bool more;
-    const char *from_a = nullptr, *from_b = nullptr;          // its next stage, of which `left` values of c are there
-    int left = 0, to_load = 0, to_slot = 0;                   // stages of it still to be asked for
-    auto begin = [&] {
-        more = next(ahead);
-        if (!more) {
-            left = 0, to_load = INT32_MAX;
-            return;
-        }
+    bool more = true;
+    auto begin_a = [&] {
+        if (!Sh::kLeadB) more = next(ahead);
         const int l = anew(lane);
-#pragma unroll
-        for (int i = 0; i < Sh::kLoadsA; ++i) A::lane_at(i * Sh::kWaves + wave, l, ahead.rows_a, pitch_a, off_a[i], c_a);
-#pragma unroll
-        for (int i = 0; i < Sh::kLoadsB; ++i) B::lane_at(i * Sh::kWaves + wave, l, ahead.rows_b, pitch_b, off_b[i], c_b);
-        from_a = ahead.a, from_b = ahead.b, left = ahead.c, to_load = stages_of(ahead);
+        if (more) ra.begin(ahead.a, ahead.rows_a, ahead.c, stages_of(ahead), l, wave);
+        else ra.end();
     };
-    auto load = [&] {                                         // behind the last tile it asks for nothing
-        if (to_load == 0) begin();
-        const int there = max(left, 0);
-        const uint32_t dst = lds_at + to_slot * Sh::kStage + wave * 1024;
-        const i32x4 ra = lds_source(from_a, (uint32_t)uniform((int)(Sh::kAcrossA ? (uint32_t)min(there, KB) * pitch_a : there ? kRecords : 0)));
-        const i32x4 rb = lds_source(from_b, (uint32_t)uniform((int)(Sh::kAcrossB ? (uint32_t)min(there, KB) * pitch_b : there ? kRecords : 0)));
-#pragma unroll
-        for (int i = 0; i < Sh::kLoadsA; ++i)
-            load_to_lds(ra, Sh::kAcrossA || c_a < there ? off_a[i] : kNowhere, dst + i * Sh::kWaves * 1024);
-#pragma unroll
-        for (int i = 0; i < Sh::kLoadsB; ++i)
-            load_to_lds(rb, Sh::kAcrossB || c_b < there ? off_b[i] : kNowhere, dst + A::kBytes + i * Sh::kWaves * 1024);
-        left -= min(left, KB);
-        from_a += left > 0 ? (Sh::kAcrossA ? (int64_t)KB * pitch_a : KB * 2) : 0;
-        from_b += left > 0 ? (Sh::kAcrossB ? (int64_t)KB * pitch_b : KB * 2) : 0;
-        --to_load;
-        to_slot = to_slot == S - 1 ? 0 : to_slot + 1;
+    auto begin_b = [&] {
+        if (Sh::kLeadB) more = next(ahead);
+        const int l = anew(lane);
+        if (more) rb.begin(ahead.b, ahead.rows_b, ahead.c, stages_of(ahead), l, wave);
+        else rb.end();
+    };
+    // The next stage of each operand; the leading one finds the next tile.
+    auto prepare_a = [&] {
+        if (ra.to_load == 0) begin_a();
+        ra.prepare();
+    };
+    auto prepare_b = [&] {
+        if (rb.to_load == 0) begin_b();
+        rb.prepare();
+    };
+    auto prepare = [&] {
+        if (Sh::kLeadB) prepare_b(), prepare_a();
+        else prepare_a(), prepare_b();
+        settle(ra.source, rb.source);
+    };
+    constexpr int kLoads = Sh::kLoadsA + Sh::kLoadsB;
+    auto load = [&](int i) {                                  // the leading operand's behind the other's
+        if (Sh::kLeadB) {
+            if (i < Sh::kLoadsA) ra.load(i);
+            else rb.load(i - Sh::kLoadsA);
+        } else {
+            if (i < Sh::kLoadsB) rb.load(i);
+            else ra.load(i - Sh::kLoadsB);
+        }
     };
 
-    begin();
+    if (Sh::kLeadB) begin_b(), begin_a();
+    else begin_a(), begin_b();
     if (!more) return;
 #pragma unroll
-    for (int s = 0; s < S; ++s) load();
+    for (int s = 0; s < S; ++s) {
+        prepare();
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load(i);
+    }
+    if constexpr (SA > S) {
+        ra.prepare();
+        settle(ra.source, rb.source);
+#pragma unroll
+        for (int i = 0; i < Sh::kLoadsA; ++i) ra.load(i);
+    }
+    if constexpr (SB > S) {
+        rb.prepare();
+        settle(ra.source, rb.source);
+#pragma unroll
+        for (int i = 0; i < Sh::kLoadsB; ++i) rb.load(i);
+    }
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    int slot = 0;
+    int slot_a = 0, slot_b = 0;
 
     // A tile of which this wavefront has `blocks` blocks of rows.
-    auto take = [&](const Work &w, auto blocks) {
+    auto take = [&](const Work &w, auto blocks, auto with_bias) {
         constexpr int MB = decltype(blocks)::value, MR = MB ? MB : 1, Q = KB / 16;
         const int stages = stages_of(w);
         f32x16 acc[MR][NJ];
@@ -461,36 +515,40 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, S, KB>::kW
             for (int n = 0; n < NJ; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[m][n][r] = 0;
-        float bias_part[MR] = {};                             // weights: sums of dy's columns, this wavefront's share of c
-        int sum_bias = JOB == Job::weights && g.d_bias && w.j0 == 0;
+        // Sums of dy's columns (weights, the tiles of the first columns of x); of the wavefronts that have the same rows the one with column m % WJ sums block m.
+        constexpr bool BIAS = decltype(with_bias)::value;
+        constexpr int kShare = (MR + WJ - 1) / WJ;
+        float bias_part[kShare] = {};
 
         // Fragments of 16 values of c are read one step of products ahead, the first ones of a stage behind the barrier that says that the stage is
         // there; that stands in front of the last products of the stage before, so that nobody waits for LDS with idle matrix cores.
         bf16x8 fa[2][MR], fb[2][NJ];
         auto fetch = [&](int q, int to) {
             if constexpr (MB > 0) {
-                const char *ta = lds + slot * Sh::kStage, *tb = ta + A::kBytes;
+                const char *ta = lds + slot_a * A::kBytes, *tb = lds + SA * A::kBytes + slot_b * B::kBytes;
 #pragma unroll
                 for (int n = 0; n < NJ; ++n) fb[to][n] = B::fragment(tb, lane, wj * NJ + n, q);
 #pragma unroll
                 for (int m = 0; m < MB; ++m) fa[to][m] = A::fragment(ta, lane, m * WI + wi, q);
             }
         };
-        auto products = [&](int t, int q) {
+        // One block of rows' products of a step.
+        auto block = [&](int q, int m) {
             const int of = q & 1;
 #pragma unroll
-            for (int m = 0; m < MB; ++m)
+            for (int n = 0; n < NJ; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[of][n], fa[of][m], acc[m][n], 0, 0, 0);
+        };
+        // A wavefront's share is read for it a second time: its number is not known to the compiler, and registers have no index.
+        auto add_bias = [&](int q) {
+            if constexpr (BIAS && MB > 0) {
+                const char *ta = lds + slot_a * A::kBytes;
 #pragma unroll
-                for (int n = 0; n < NJ; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[of][n], fa[of][m], acc[m][n], 0, 0, 0);
-            if (JOB == Job::weights) sum_bias = hidden(sum_bias);
-            if (JOB == Job::weights && sum_bias && (t * Q + q) % WJ == wj) {
-#pragma unroll
-                for (int m = 0; m < MB; ++m) {
-                    const F8 f = widen(fa[of][m]);
-                    bias_part[m] += ((f.v[0] + f.v[1]) + (f.v[2] + f.v[3])) + ((f.v[4] + f.v[5]) + (f.v[6] + f.v[7]));
+                for (int k = 0; k < kShare; ++k) {
+                    const int m = wj + k * WJ;
+                    const F8 f = widen(A::fragment(ta, lane, (m < MB ? m : 0) * WI + wi, q));
+                    bias_part[k] += ((f.v[0] + f.v[1]) + (f.v[2] + f.v[3])) + ((f.v[4] + f.v[5]) + (f.v[6] + f.v[7]));
                 }
             }
-            __builtin_amdgcn_sched_barrier(0);
         };
         // The next stage is there, and nobody reads this one any more.  The first S stages of a tile are there when it begins: they are waited for in front of
         // the stores of the tile before, so that no wait for them is one for stores.
@@ -498,7 +556,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, S, KB>::kW
         auto arrived = [&] {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             there = hidden(there - 1);
-            if (there < 0) wait_loads<(S - 2) * (Sh::kLoadsA + Sh::kLoadsB)>();
+            if (there < 0) wait_loads<Sh::kLater>();
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         };
@@ -508,16 +566,31 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, S, KB>::kW
 #pragma unroll
             for (int q = 0; q < Q - 1; ++q) {
                 fetch(q + 1, q + 1 & 1);
-                products(t, q);
+#pragma unroll
+                for (int m = 0; m < MB; ++m) block(q, m);
+                add_bias(q);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            slot = slot == S - 1 ? 0 : slot + 1;
+            add_bias(Q - 1);
+            slot_a = slot_a == SA - 1 ? 0 : slot_a + 1;
+            slot_b = slot_b == SB - 1 ? 0 : slot_b + 1;
+            prepare();
             arrived();
-            load();
             if (t + 1 < stages) fetch(0, 0);                  // the next tile's first are read when it begins
-            products(t, Q - 1);
+            // The loads of the stage that takes this one's place, between the products of its last step.
+            constexpr int kEach = (kLoads + MR - 1) / MR;
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+#pragma unroll
+                for (int i = m * kEach; i < (m + 1) * kEach && i < kLoads; ++i) load(i);
+                if (MB > 0) block(Q - 1, m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
 
-        // ---- results.  A lane holds four times four consecutive columns of one row of a block, and lane ^ 32 the four beside them; exchanged, it holds twice eight.
+        // ---- results.  A lane holds four times four consecutive columns of one row of a block, lane ^ 32 the four beside them.  Two exchanges, between
+        // halves and between quarters of the wavefront, leave it with eight consecutive columns of one row of the block's upper half and eight of the lower:
+        // four lanes hold 64 consecutive bytes in bf16, which is what is read and written beside them, too.
         const Act act(g.activation);
         const int size = g.out32 ? 4 : 2;
         // What a call has beside the result; the compiler is kept from making a copy of all this for each of the possibilities.
@@ -526,97 +599,141 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, S, KB>::kW
         const __amdgpu_buffer_rsrc_t rp = make_rsrc(g.pre + ((int64_t)w.i0 * g.ld_pre + w.j0) * 2, kRecords);
         const __amdgpu_buffer_rsrc_t rr = make_rsrc(g.residual + ((int64_t)w.i0 * g.ld_res + w.j0) * size, kRecords);
         const __amdgpu_buffer_rsrc_t rb = make_rsrc(g.bias + (JOB == Job::product ? (int64_t)w.group * g.N + w.j0 : 0), kRecords);
+        const int l = anew(lane), quarter = l >> 4;
+        const int col0 = wj * NJ * 32 + (quarter & 1) * 16 + (quarter >> 1) * 8;              // of block n: + 32 n
+        auto row_of = [&](int m, int half) { return (m * WI + wi) * 32 + half * 16 + (l & 15); };
+        auto place = [&](int m, int n, int half, int64_t ld) {                                // in values
+            const int i = row_of(m, half), j = col0 + n * 32;
+            return i < w.rows_a && j < w.rows_b ? i * (uint32_t)ld + j : kNone;
+        };
+        // Beside the result is read: the bias of the tile's columns, and for each row `pre` (input, a block of rows ahead) or the residual (what an
+        // fp32 one has more than 16 bytes of, where it is used).
+        F8 bias[NJ];
+        if (JOB == Job::product && has_bias) {
+#pragma unroll
+            for (int n = 0; n < NJ; ++n) bias[n] = read8(rb, col0 + n * 32 < w.rows_b ? (uint32_t)(col0 + n * 32) : kNone, true);
+        }
+        constexpr int kAhead = JOB == Job::input ? 1 : 0;     // blocks of rows (a product's bias has the registers of a second one)
+        i32x4 beside[kAhead + 1][NJ * 2];
+        const int reads = JOB == Job::input ? has_pre : has_residual;
+        auto ask = [&](int m) {
+            if (JOB == Job::weights || !reads) return;
+#pragma unroll
+            for (int p = 0; p < NJ * 2; ++p) {
+                if constexpr (JOB == Job::input) {
+                    const uint32_t at = place(m, p / 2, p % 2, g.ld_pre);
+                    beside[m & kAhead][p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, (int)(at == kNone ? kNowhere : at * 2), 0, 0));
+                } else {
+                    const uint32_t at = place(m, p / 2, p % 2, g.ld_res);
+                    beside[m & kAhead][p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, (int)(at == kNone ? kNowhere : at * size), 0, 0));
+                }
+            }
+        };
+        if constexpr (MB > 0 && kAhead > 0) ask(0);
         wait_loads<0>();
-        const int l = anew(lane);
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
-            const int i = (m * WI + wi) * 32 + (l & 31);
+            if (m + kAhead < MB) ask(m + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int n = 0; n < NJ; ++n)
+            for (int n = 0; n < NJ; ++n) {
+                F8 f[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int j = (wj * NJ + n) * 32 + h * 16 + (l >> 5) * 8;
-                    const bool in = i < w.rows_a && j < w.rows_b;
-                    has_bias = hidden(has_bias), has_pre = hidden(has_pre), has_residual = hidden(has_residual), out32 = hidden(out32), kind = hidden(kind);
-                    F8 f;
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float lo = acc[m][n][h * 8 + e], hi = acc[m][n][h * 8 + 4 + e];
                         const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi), false, false);
                         const uint32_t first = both[0], second = both[1];
-                        f.v[e] = __builtin_bit_cast(float, first);
-                        f.v[4 + e] = __builtin_bit_cast(float, second);
+                        f[h].v[e] = __builtin_bit_cast(float, first);
+                        f[h].v[4 + e] = __builtin_bit_cast(float, second);
                     }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float lo = f[0].v[e], hi = f[1].v[e];
+                    const auto both = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi), false, false);
+                    const uint32_t first = both[0], second = both[1];
+                    f[0].v[e] = __builtin_bit_cast(float, first);
+                    f[1].v[e] = __builtin_bit_cast(float, second);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    has_bias = hidden(has_bias), has_pre = hidden(has_pre), has_residual = hidden(has_residual), out32 = hidden(out32), kind = hidden(kind);
+                    F8 &v = f[h];
                     if constexpr (JOB == Job::product) {
                         if (has_bias) {
-                            const F8 b = read8(rb, j < w.rows_b ? (uint32_t)j : kNone, true);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) f.v[e] += b.v[e];
+                            for (int e = 0; e < 8; ++e) v.v[e] += bias[n].v[e];
                         }
-                        if (has_pre) write8(rp, in ? i * (uint32_t)g.ld_pre + j : kNone, false, f);
+                        if (has_pre) write8(rp, place(m, n, h, g.ld_pre), false, v);
                         if (kind >= kActGelu) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) f.v[e] = act.smooth(f.v[e]);
+                            for (int e = 0; e < 8; ++e) v.v[e] = act.smooth(v.v[e]);
                         } else if (kind == kActRelu) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) f.v[e] = relu_of(f.v[e]);
+                            for (int e = 0; e < 8; ++e) v.v[e] = relu_of(v.v[e]);
                         }
                         if (has_residual) {
-                            const F8 s = read8(rr, in ? i * (uint32_t)g.ld_res + j : kNone, out32);
+                            const i32x4 low = beside[m & kAhead][n * 2 + h];
+                            F8 s = widen(__builtin_bit_cast(bf16x8, low));
+                            if (out32) {
+                                const uint32_t at = place(m, n, h, g.ld_res);
+                                const f32x4 a = __builtin_bit_cast(f32x4, low);
+                                const f32x4 b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, (int)(at == kNone ? kNowhere : at * 4), 16, 0));
+                                s = F8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+                            }
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) f.v[e] += s.v[e];
+                            for (int e = 0; e < 8; ++e) v.v[e] += s.v[e];
                         }
                     } else if constexpr (JOB == Job::input) {
                         if (has_pre) {
-                            const F8 s = read8(rp, in ? i * (uint32_t)g.ld_pre + j : kNone, false);
+                            const i32x4 low = beside[m & kAhead][n * 2 + h];
+                            const F8 s = widen(__builtin_bit_cast(bf16x8, low));
                             if (kind >= kActGelu) {
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) f.v[e] *= act.smooth_slope(s.v[e]);
+                                for (int e = 0; e < 8; ++e) v.v[e] *= act.smooth_slope(s.v[e]);
                             } else if (kind == kActRelu) {
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) f.v[e] *= relu_slope(s.v[e]);
+                                for (int e = 0; e < 8; ++e) v.v[e] *= relu_slope(s.v[e]);
                             }
                         }
                     }
-                    write8(ro, in ? i * (uint32_t)g.ldo + j : kNone, out32, f);
+                    write8(ro, place(m, n, h, g.ldo), out32, v);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-        }
-        if (JOB == Job::weights && sum_bias) {                // the wavefronts' shares of a column, in a fixed order
-            float *part = reinterpret_cast<float *>(lds + S * Sh::kStage);   // [WJ][2][BM]
-#pragma unroll
-            for (int m = 0; m < MB; ++m) part[(wj * 2 + (l >> 5)) * Sh::BM + (m * WI + wi) * 32 + (l & 31)] = bias_part[m];
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
-            for (int i = tid; i < w.rows_a; i += Sh::kThreads) {
-                float sum = 0;
-                for (int p = 0; p < 2 * WJ; ++p) sum += part[p * Sh::BM + i];
-                g.d_bias[(int64_t)w.group * g.N + w.i0 + i] = sum;
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
         }
+        if constexpr (BIAS && MB > 0) {
+#pragma unroll
+            for (int k = 0; k < kShare; ++k) {
+                const float sum = bias_part[k] + __shfl_xor(bias_part[k], 32);
+                const int m = wj + k * WJ, i = (m * WI + wi) * 32 + (l & 31);
+                if (m < MB && l < 32 && i < w.rows_a) g.d_bias[(int64_t)w.group * g.N + w.i0 + i] = sum;
+            }
+        }
+    };
+    auto take_blocks = [&](const Work &w, auto with_bias) {
+        const int blocks = ((w.rows_a + 31) / 32 - wi + WI - 1) / WI;
+        if (blocks <= 0) take(w, Int<0>(), with_bias);
+        else if (MI == 1 || blocks == 1) take(w, Int<1>(), with_bias);
+        else if (MI == 2 || blocks == 2) take(w, Int<(MI < 2 ? MI : 2)>(), with_bias);
+        else if (MI == 3 || blocks == 3) take(w, Int<(MI < 3 ? MI : 3)>(), with_bias);
+        else take(w, Int<MI>(), with_bias);
     };
     while (true) {
         const Work w = ahead;
-        const int blocks = ((w.rows_a + 31) / 32 - wi + WI - 1) / WI;
-        if (blocks <= 0) take(w, Int<0>());
-        else if (MI == 1 || blocks == 1) take(w, Int<1>());
-        else if (MI == 2 || blocks == 2) take(w, Int<(MI < 2 ? MI : 2)>());
-        else if (MI == 3 || blocks == 3) take(w, Int<(MI < 3 ? MI : 3)>());
-        else take(w, Int<MI>());
+        if (JOB == Job::weights && g.d_bias && w.j0 == 0) take_blocks(w, std::bool_constant<JOB == Job::weights>());
+        else take_blocks(w, std::false_type());
         if (!more) break;
     }
 }
 
-template <Job JOB, int WI, int WJ, int MI, int NJ, int S, int KB>
+template <Job JOB, int WI, int WJ, int MI, int NJ, int SA, int SB, int KB>
 int launch_shape(const GemmArgs &g, hipStream_t st)
 {
-    typedef Shape<JOB, WI, WJ, MI, NJ, S, KB> Sh;
+    typedef Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB> Sh;
     static LdsGrant grant;
-    const void *kernel = (const void *)expert_gemm_tiles<JOB, WI, WJ, MI, NJ, S, KB>;
+    const void *kernel = (const void *)expert_gemm_tiles<JOB, WI, WJ, MI, NJ, SA, SB, KB>;
     const int e = allow_lds(grant, kernel, Sh::kLds);
     if (e) return e;
     int64_t tiles;                                            // at most
@@ -627,7 +744,7 @@ int launch_shape(const GemmArgs &g, hipStream_t st)
         tiles = (int64_t)(g.M / Sh::BM + (g.groups < g.M ? g.groups : g.M)) * ((cols + Sh::BN - 1) / Sh::BN);
     }
     const int64_t most = Sh::kPerUnit * stream_compute_units(st), grid = tiles < most ? (tiles + 7) / 8 * 8 : most;
-    expert_gemm_tiles<JOB, WI, WJ, MI, NJ, S, KB><<<(uint32_t)grid, Sh::kThreads, Sh::kLds, st>>>(g);
+    expert_gemm_tiles<JOB, WI, WJ, MI, NJ, SA, SB, KB><<<(uint32_t)grid, Sh::kThreads, Sh::kLds, st>>>(g);
     return (int)hipGetLastError();
 }
 
@@ -647,7 +764,7 @@ int launch_expert_gemm(const ExpertGemmShape &s, const void *x, int64_t ldx, int
     g.a = (const char *)x, g.lda = ldx, g.b = (const char *)w, g.ldb = s.K, g.b_group = (int64_t)s.N * s.K;
     g.bias = bias, g.pre = (char *)pre, g.ld_pre = ld_pre, g.residual = (const char *)residual, g.ld_res = ld_res;
     g.out = (char *)y, g.ldo = ldy;
-    return launch_shape<Job::product, 2, 4, 4, 2, 2, 64>(g, st);
+    return launch_shape<Job::product, 2, 4, 4, 2, 2, 3, 64>(g, st);
 }
 
 int launch_expert_gemm_input(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, int32_t M, const void *w, const int32_t *offsets, const void *pre,
@@ -657,7 +774,7 @@ int launch_expert_gemm_input(const ExpertGemmShape &s, const void *dy, int64_t l
     g.a = (const char *)dy, g.lda = ld_dy, g.b = (const char *)w, g.ldb = s.K, g.b_group = (int64_t)s.N * s.K;
     g.pre = (char *)const_cast<void *>(pre), g.ld_pre = ld_pre;
     g.out = (char *)dx, g.ldo = ld_dx;
-    return launch_shape<Job::input, 2, 4, 4, 2, 2, 64>(g, st);
+    return launch_shape<Job::input, 2, 4, 4, 2, 2, 3, 64>(g, st);
 }
 
 int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, int32_t M, const int32_t *offsets,
@@ -666,7 +783,7 @@ int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t
     GemmArgs g = args_of(s, offsets, M);
     g.a = (const char *)dy, g.lda = ld_dy, g.b = (const char *)x, g.ldb = ldx;
     g.out = (char *)dw, g.ldo = s.K, g.out_group = (int64_t)s.N * s.K, g.d_bias = d_bias;
-    return launch_shape<Job::weights, 2, 4, 4, 2, 2, 64>(g, st);
+    return launch_shape<Job::weights, 2, 4, 4, 2, 2, 3, 64>(g, st);
 }
 
 }  // namespace sida
