@@ -226,7 +226,9 @@ int sida_expert_gemm_input(const sida_expert_gemm_config *c, const void *dy_dev,
 
 size_t sida_expert_gemm_weights_workspace_bytes(const sida_expert_gemm_config *c, int32_t M)
 {
-    return expert_cfg_ok(c, M) ? 0 : 0;
+    if (!expert_cfg_ok(c, M)) return 0;
+    const int chunk = expert_weights_chunk(M, c->groups, c->N, c->K);
+    return chunk ? up((size_t)expert_weights_parts(M, c->groups, chunk) * c->N * (c->K + 1) * 4, 256) : 0;
 }
 
 int sida_expert_gemm_weights(const sida_expert_gemm_config *c, const void *dy_dev, int64_t ld_dy, const void *x_dev, int64_t ldx, int32_t M,

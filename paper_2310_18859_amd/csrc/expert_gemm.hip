@@ -25,7 +25,7 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 
-enum class Job { product, input, weights };
+enum class Job { product, input, weights, parts };           // parts: the weights' gradient of `chunk` rows at a time, to be added up
 
 struct GemmArgs {
     const char *a, *b;           // rows (product: x, input: dy, weights: dy) and the other operand (W, W, x)
@@ -41,6 +41,7 @@ struct GemmArgs {
     const char *residual;
     int64_t ld_pre, ld_res;
     float *d_bias;               // weights
+    int chunk;                   // parts: rows of a part
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, uint32_t bytes)
@@ -95,7 +96,7 @@ struct Work {
     const char *a, *b;           // the tile's first row, at c = 0
     int rows_a, rows_b, c;       // rows of the tile that are there, length of the sum
     int i0, j0;                  // first row and column of the result
-    int group;
+    int group, to;               // to (weights): which of the result's matrices, the group's or the part's
 };
 
 // The items that workgroup b takes one after the other, of `total`: b runs on XCD b % 8, and an XCD takes `block` items in a row of every eight
@@ -147,11 +148,10 @@ struct Groups {
     }
 };
 
-// Row tiles are counted group by group; a lane knows how many there are up to its last group.
-template <int BM>
+// Row tiles of `tall` rows are counted group by group; a lane knows how many there are up to its last group.
 struct RowTiles : Groups {
-    int upto, total;
-    __device__ __forceinline__ explicit RowTiles(const GemmArgs &g) : Groups(g)
+    int tall, upto, total;
+    __device__ __forceinline__ RowTiles(const GemmArgs &g, int tall_) : Groups(g), tall(tall_)
     {
         const int lane = threadIdx.x & 63;
         upto = tiles();
@@ -162,8 +162,9 @@ struct RowTiles : Groups {
         }
         total = __builtin_amdgcn_readlane(upto, 63);
     }
-    __device__ __forceinline__ int tiles_of(int i) const { return (max(0, at[i + 1] - at[i]) + BM - 1) / BM; }
+    __device__ __forceinline__ int tiles_of(int i) const { return (max(0, at[i + 1] - at[i]) + tall - 1) / tall; }
     __device__ __forceinline__ int tiles() const { return tiles_of(0) + tiles_of(1) + tiles_of(2) + tiles_of(3); }
+    // Of row tile mt: its group, first row and number of rows.
     __device__ __forceinline__ void find(int mt, int &group_of, int &row0_of, int &rows_of) const
     {
         const int owner = __builtin_ctzll(__ballot(upto > mt));
@@ -173,8 +174,8 @@ struct RowTiles : Groups {
             const int n = tiles_of(i);
             if (left >= 0 && left < n) {
                 group = (threadIdx.x & 63) * 4 + i;
-                row0 = at[i] + left * BM;
-                rows = min(BM, at[i + 1] - row0);
+                row0 = at[i] + left * tall;
+                rows = min(tall, at[i + 1] - row0);
             }
             left -= n;
         }
@@ -182,8 +183,19 @@ struct RowTiles : Groups {
         row0_of = __builtin_amdgcn_readlane(row0, owner);
         rows_of = __builtin_amdgcn_readlane(rows, owner);
     }
+    // Of a group: its first row tile and how many it has.
+    __device__ __forceinline__ void of(int group, int &first, int &n) const
+    {
+        int before = upto - tiles(), mine = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            before += i < (group & 3) ? tiles_of(i) : 0;
+            mine = i == (group & 3) ? tiles_of(i) : mine;
+        }
+        first = __builtin_amdgcn_readlane(before, group >> 2);
+        n = __builtin_amdgcn_readlane(mine, group >> 2);
+    }
 };
-
 
 // The groups by their number of rows, the largest first; the lower of equal ones.  Four to a lane, a byte each.
 template <int THREADS>
@@ -303,6 +315,26 @@ __device__ __forceinline__ F8 widen(bf16x8 x)
     for (int i = 0; i < 8; ++i) f.v[i] = (float)x[i];
     return f;
 }
+__device__ __forceinline__ void activate(const Act &act, int kind, F8 &f)
+{
+    if (kind >= kActGelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.v[e] = act.smooth(f.v[e]);
+    } else if (kind == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.v[e] = relu_of(f.v[e]);
+    }
+}
+__device__ __forceinline__ void times_slope(const Act &act, int kind, F8 &f, const F8 &pre)
+{
+    if (kind >= kActGelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.v[e] *= act.smooth_slope(pre.v[e]);
+    } else if (kind == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.v[e] *= relu_slope(pre.v[e]);
+    }
+}
 // Eight values from `at`, in values; kNone: none (zeros, nothing stored).
 constexpr uint32_t kNone = kNowhere;
 __device__ __forceinline__ F8 read8(__amdgpu_buffer_rsrc_t r, uint32_t at, bool f32)
@@ -332,7 +364,7 @@ __device__ __forceinline__ void write8(__amdgpu_buffer_rsrc_t r, uint32_t at, bo
 // SA and SB stages of KB values of c of the two operands in LDS.
 template <Job JOB, int WI, int WJ, int MI, int NJ, int SA, int SB, int KB>
 struct Shape {
-    static constexpr bool kAcrossA = JOB == Job::weights, kAcrossB = JOB != Job::product;
+    static constexpr bool kAcrossA = JOB == Job::weights || JOB == Job::parts, kAcrossB = JOB != Job::product;
     static constexpr int kWaves = WI * WJ, kThreads = kWaves * 64;
     static constexpr int BM = 32 * MI * WI, BN = 32 * NJ * WJ;
     typedef Tile<kAcrossA, BM, KB> A;
@@ -403,26 +435,39 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
     const int cols = JOB == Job::product ? g.N : g.K, col_tiles = (cols + Sh::BN - 1) / Sh::BN;
 
     // ---- the tiles
-    const std::conditional_t<JOB == Job::weights, Groups, RowTiles<Sh::BM>> rows(g);
-    const int tiles_i = JOB == Job::weights ? (g.N + Sh::BM - 1) / Sh::BM : 0;
+    constexpr bool kWeights = Sh::kAcrossA;
+    const int tiles_i = kWeights ? (g.N + Sh::BM - 1) / Sh::BM : 0;
+    std::conditional_t<JOB == Job::weights, Groups, RowTiles> rows = [&] {
+        if constexpr (JOB == Job::weights) return Groups(g);
+        else return RowTiles(g, JOB == Job::parts ? g.chunk : Sh::BM);
+    }();
     uint32_t order = 0;
-    if constexpr (JOB == Job::weights) order = groups_by_rows<Sh::kThreads>(rows, g.groups, lds);
     int64_t total;
-    if constexpr (JOB == Job::weights) total = (int64_t)g.groups * tiles_i * col_tiles;
-    else total = (int64_t)rows.total * col_tiles;
+    if constexpr (JOB == Job::weights) {
+        order = groups_by_rows<Sh::kThreads>(rows, g.groups, lds);
+        total = (int64_t)g.groups * tiles_i * col_tiles;
+    } else {
+        total = (int64_t)rows.total * col_tiles * (JOB == Job::parts ? tiles_i : 1);
+    }
     Items items(total, gridDim.x, 64);
     auto next = [&](Work &w) {
         const int id = items.next();
         if (id < 0) return false;
-        if constexpr (JOB == Job::weights) {
+        if constexpr (kWeights) {
             const int at = id / (tiles_i * col_tiles), tile = id % (tiles_i * col_tiles);
-            w.group = __builtin_amdgcn_readlane(order, at >> 2) >> (at & 3) * 8 & 255;
             int from;
-            rows.rows(w.group, from, w.c);
+            if constexpr (JOB == Job::weights) {
+                w.to = w.group = __builtin_amdgcn_readlane(order, at >> 2) >> (at & 3) * 8 & 255;
+                rows.rows(w.group, from, w.c);
+            } else {
+                w.to = at;
+                rows.find(at, w.group, from, w.c);
+            }
             w.i0 = tile / col_tiles * Sh::BM, w.j0 = tile % col_tiles * Sh::BN;
             w.a = g.a + ((int64_t)from * g.lda + w.i0) * 2, w.b = g.b + ((int64_t)from * g.ldb + w.j0) * 2;
             w.rows_a = min(Sh::BM, g.N - w.i0);
         } else {
+            w.to = 0;
             rows.find(id / col_tiles, w.group, w.i0, w.rows_a);
             w.j0 = id % col_tiles * Sh::BN;
             w.a = g.a + (int64_t)w.i0 * g.lda * 2;
@@ -430,7 +475,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
             w.c = JOB == Job::product ? g.K : g.N;
         }
         w.rows_b = min(Sh::BN, cols - w.j0);
-        w = Work{uniform(w.a), uniform(w.b), uniform(w.rows_a), uniform(w.rows_b), uniform(w.c), uniform(w.i0), uniform(w.j0), uniform(w.group)};
+        w = Work{uniform(w.a), uniform(w.b), uniform(w.rows_a), uniform(w.rows_b), uniform(w.c), uniform(w.i0), uniform(w.j0), uniform(w.group), uniform(w.to)};
         return true;
     };
     auto stages_of = [&](const Work &w) { return max(Sh::kMost, (w.c + KB - 1) / KB); };
@@ -507,7 +552,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
     // A tile of which this wavefront has `blocks` blocks of rows.
     auto take = [&](const Work &w, auto blocks, auto with_bias) {
         constexpr int MB = decltype(blocks)::value, MR = MB ? MB : 1, Q = KB / 16;
-        const int stages = stages_of(w);
+        const int stages = stages_of(w), whole = (w.c + KB - 1) / KB;                         // those that hold something
         f32x16 acc[MR][NJ];
 #pragma unroll
         for (int m = 0; m < MB; ++m)
@@ -560,30 +605,32 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         };
-        fetch(0, 0);
+        if (whole > 0) fetch(0, 0);
 #pragma clang loop unroll(disable)
         for (int t = 0; t < stages; ++t) {
+            if (t < whole) {
 #pragma unroll
-            for (int q = 0; q < Q - 1; ++q) {
-                fetch(q + 1, q + 1 & 1);
+                for (int q = 0; q < Q - 1; ++q) {
+                    fetch(q + 1, q + 1 & 1);
 #pragma unroll
-                for (int m = 0; m < MB; ++m) block(q, m);
-                add_bias(q);
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int m = 0; m < MB; ++m) block(q, m);
+                    add_bias(q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                add_bias(Q - 1);
             }
-            add_bias(Q - 1);
             slot_a = slot_a == SA - 1 ? 0 : slot_a + 1;
             slot_b = slot_b == SB - 1 ? 0 : slot_b + 1;
             prepare();
             arrived();
-            if (t + 1 < stages) fetch(0, 0);                  // the next tile's first are read when it begins
+            if (t + 1 < whole) fetch(0, 0);                   // the next tile's first are read when it begins
             // The loads of the stage that takes this one's place, between the products of its last step.
             constexpr int kEach = (kLoads + MR - 1) / MR;
 #pragma unroll
             for (int m = 0; m < MR; ++m) {
 #pragma unroll
                 for (int i = m * kEach; i < (m + 1) * kEach && i < kLoads; ++i) load(i);
-                if (MB > 0) block(Q - 1, m);
+                if (MB > 0 && t < whole) block(Q - 1, m);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -595,7 +642,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
         const int size = g.out32 ? 4 : 2;
         // What a call has beside the result; the compiler is kept from making a copy of all this for each of the possibilities.
         int has_bias = g.bias != nullptr, has_pre = g.pre != nullptr, has_residual = g.residual != nullptr, out32 = g.out32, kind = act.kind;
-        const __amdgpu_buffer_rsrc_t ro = make_rsrc(g.out + ((JOB == Job::weights ? w.group * g.out_group : 0) + (int64_t)w.i0 * g.ldo + w.j0) * size, kRecords);
+        const __amdgpu_buffer_rsrc_t ro = make_rsrc(g.out + ((kWeights ? w.to * g.out_group : 0) + (int64_t)w.i0 * g.ldo + w.j0) * size, kRecords);
         const __amdgpu_buffer_rsrc_t rp = make_rsrc(g.pre + ((int64_t)w.i0 * g.ld_pre + w.j0) * 2, kRecords);
         const __amdgpu_buffer_rsrc_t rr = make_rsrc(g.residual + ((int64_t)w.i0 * g.ld_res + w.j0) * size, kRecords);
         const __amdgpu_buffer_rsrc_t rb = make_rsrc(g.bias + (JOB == Job::product ? (int64_t)w.group * g.N + w.j0 : 0), kRecords);
@@ -617,7 +664,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
         i32x4 beside[kAhead + 1][NJ * 2];
         const int reads = JOB == Job::input ? has_pre : has_residual;
         auto ask = [&](int m) {
-            if (JOB == Job::weights || !reads) return;
+            if (kWeights || !reads) return;
 #pragma unroll
             for (int p = 0; p < NJ * 2; ++p) {
                 if constexpr (JOB == Job::input) {
@@ -666,13 +713,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
                             for (int e = 0; e < 8; ++e) v.v[e] += bias[n].v[e];
                         }
                         if (has_pre) write8(rp, place(m, n, h, g.ld_pre), false, v);
-                        if (kind >= kActGelu) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v.v[e] = act.smooth(v.v[e]);
-                        } else if (kind == kActRelu) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v.v[e] = relu_of(v.v[e]);
-                        }
+                        activate(act, kind, v);
                         if (has_residual) {
                             const i32x4 low = beside[m & kAhead][n * 2 + h];
                             F8 s = widen(__builtin_bit_cast(bf16x8, low));
@@ -688,14 +729,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
                     } else if constexpr (JOB == Job::input) {
                         if (has_pre) {
                             const i32x4 low = beside[m & kAhead][n * 2 + h];
-                            const F8 s = widen(__builtin_bit_cast(bf16x8, low));
-                            if (kind >= kActGelu) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) v.v[e] *= act.smooth_slope(s.v[e]);
-                            } else if (kind == kActRelu) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) v.v[e] *= relu_slope(s.v[e]);
-                            }
+                            times_slope(act, kind, v, widen(__builtin_bit_cast(bf16x8, low)));
                         }
                     }
                     write8(ro, place(m, n, h, g.ldo), out32, v);
@@ -708,7 +742,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
             for (int k = 0; k < kShare; ++k) {
                 const float sum = bias_part[k] + __shfl_xor(bias_part[k], 32);
                 const int m = wj + k * WJ, i = (m * WI + wi) * 32 + (l & 31);
-                if (m < MB && l < 32 && i < w.rows_a) g.d_bias[(int64_t)w.group * g.N + w.i0 + i] = sum;
+                if (m < MB && l < 32 && i < w.rows_a) g.d_bias[(int64_t)w.to * g.N + w.i0 + i] = sum;
             }
         }
     };
@@ -722,10 +756,147 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
     };
     while (true) {
         const Work w = ahead;
-        if (JOB == Job::weights && g.d_bias && w.j0 == 0) take_blocks(w, std::bool_constant<JOB == Job::weights>());
+        if (kWeights && g.d_bias && w.j0 == 0) take_blocks(w, std::bool_constant<kWeights>());
         else take_blocks(w, std::false_type());
         if (!more) break;
     }
+}
+
+// Few rows, few tiles: what counts is how long the way through the sum is.  A workgroup takes 32 rows and 32 columns, and its eight wavefronts share the
+// sum, 64 values of c at a time in turn, each with a ring of its own in LDS and no barrier; their parts meet in LDS and are added in a fixed order.
+constexpr int kFewWaves = 8, kFewStages = 2;
+template <Job JOB>
+__global__ __launch_bounds__(kFewWaves * 64) void expert_gemm_few(const GemmArgs g)
+{
+    constexpr bool kAcross = JOB == Job::input;
+    typedef Tile<false, 32, 64> A;
+    typedef Tile<kAcross, 32, 64> B;
+    constexpr int kStage = A::kBytes + B::kBytes, kLoads = A::kLoads, kPitch = 36;
+    static_assert(A::kLoads == B::kLoads, "loads");
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int cols = JOB == Job::product ? g.N : g.K, col_tiles = (cols + 31) / 32, length = JOB == Job::product ? g.K : g.N;
+    const RowTiles rows(g, 32);
+    Items items((int64_t)rows.total * col_tiles, gridDim.x, 64);
+    const int id = items.next();
+    if (id < 0) return;
+    int group, i0, n_rows;
+    rows.find(id / col_tiles, group, i0, n_rows);
+    const int j0 = id % col_tiles * 32, n_cols = min(32, cols - j0);
+    const uint32_t pitch_a = (uint32_t)g.lda * 2, pitch_b = (uint32_t)g.ldb * 2;
+    const char *a = uniform(g.a + (int64_t)i0 * g.lda * 2);
+    const char *b = uniform(g.b + (group * g.b_group + (JOB == Job::product ? j0 * g.ldb : (int64_t)j0)) * 2);
+    uint32_t off_a[kLoads], off_b[kLoads];
+    int c_a[kLoads], c_b[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        A::lane_at(i, lane, n_rows, pitch_a, off_a[i], c_a[i]);
+        B::lane_at(i, lane, n_cols, pitch_b, off_b[i], c_b[i]);
+    }
+    char *mine = lds + wave * kFewStages * kStage;
+    const uint32_t at = (uint32_t)uniform((int)(uintptr_t)(__attribute__((address_space(3))) char *)mine);
+    auto load = [&](int s) {                                  // this wavefront's stage s; past the end it asks for nothing
+        const int c0 = (s * kFewWaves + wave) * 64, there = max(0, min(64, length - c0));
+        i32x4 from_a = lds_source(a + (there ? c0 * 2 : 0), (uint32_t)uniform(there ? (int)kRecords : 0));
+        i32x4 from_b = lds_source(b + (there ? (kAcross ? c0 * (int64_t)pitch_b : c0 * 2) : 0), (uint32_t)uniform((int)(kAcross ? there * pitch_b : there ? kRecords : 0)));
+        settle(from_a, from_b);
+        const uint32_t dst = at + s % kFewStages * kStage;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            load_to_lds(from_a, c_a[i] < there ? off_a[i] : kNowhere, dst + i * 1024);
+            load_to_lds(from_b, kAcross || c_b[i] < there ? off_b[i] : kNowhere, dst + A::kBytes + i * 1024);
+        }
+    };
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0;
+    const int stages = (length + kFewWaves * 64 - 1) / (kFewWaves * 64);
+#pragma unroll
+    for (int s = 0; s < kFewStages; ++s) load(s);
+    for (int s = 0; s < stages; ++s) {
+        wait_loads<(kFewStages - 1) * 2 * kLoads>();
+        __builtin_amdgcn_sched_barrier(0);
+        const char *tile = mine + s % kFewStages * kStage;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(B::fragment(tile + A::kBytes, lane, 0, q), A::fragment(tile, lane, 0, q), acc, 0, 0, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // read before it is written again
+        __builtin_amdgcn_sched_barrier(0);
+        load(s + kFewStages);
+    }
+    wait_loads<0>();
+    __syncthreads();
+    float *parts = reinterpret_cast<float *>(lds);            // [wavefronts][32 rows][kPitch]
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4 *>(parts + (wave * 32 + (lane & 31)) * kPitch + q * 8 + (lane >> 5) * 4) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    const int r = tid >> 2, j = tid % 4 * 8;
+    if (r >= n_rows || j >= n_cols) return;
+    F8 f{};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+        const f32x4 *from = reinterpret_cast<const f32x4 *>(parts + (w * 32 + r) * kPitch + j);
+        const f32x4 lo = from[0], hi = from[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f.v[e] += lo[e], f.v[4 + e] += hi[e];
+    }
+    const Act act(g.activation);
+    const int size = g.out32 ? 4 : 2;
+    const __amdgpu_buffer_rsrc_t rp = make_rsrc(g.pre + ((int64_t)i0 * g.ld_pre + j0) * 2, kRecords);
+    if constexpr (JOB == Job::product) {
+        if (g.bias) {
+            const F8 bias = read8(make_rsrc(g.bias + (int64_t)group * g.N + j0, kRecords), j, true);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f.v[e] += bias.v[e];
+        }
+        if (g.pre) write8(rp, r * (uint32_t)g.ld_pre + j, false, f);
+        activate(act, act.kind, f);
+        if (g.residual) {
+            const F8 res = read8(make_rsrc(g.residual + ((int64_t)i0 * g.ld_res + j0) * size, kRecords), r * (uint32_t)g.ld_res + j, g.out32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f.v[e] += res.v[e];
+        }
+    } else {
+        if (g.pre) times_slope(act, act.kind, f, read8(rp, r * (uint32_t)g.ld_pre + j, false));
+    }
+    write8(make_rsrc(g.out + ((int64_t)i0 * g.ldo + j0) * size, kRecords), r * (uint32_t)g.ldo + j, g.out32, f);
+}
+
+// The parts of each group's gradient, added in their order; 0 for a group without rows.  Eight values to a thread; what lies behind a matrix's last are the
+// biases.
+constexpr int kAddThreads = 256;
+__global__ __launch_bounds__(kAddThreads) void expert_weights_add(const GemmArgs g, const float *parts, const float *bias_parts)
+{
+    const RowTiles rows(g, g.chunk);
+    const int64_t pieces = (int64_t)g.N * g.K / 8, all = pieces + (g.d_bias ? g.N / 8 : 0);
+    const int64_t blocks = (all + kAddThreads - 1) / kAddThreads;
+    const int group = (int)(blockIdx.x / blocks);
+    const int64_t p = blockIdx.x % blocks * kAddThreads + threadIdx.x;
+    int first, n;
+    rows.of(group, first, n);
+    if (p >= all) return;
+    const bool is_bias = p >= pieces;
+    const int64_t step = is_bias ? g.N : (int64_t)g.N * g.K, at = (is_bias ? p - pieces : p) * 8;
+    const float *from = (is_bias ? bias_parts : parts) + first * step + at;
+    F8 f{};
+    for (int c = 0; c < n; c += 4) {
+        f32x4 v[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < n) {
+                v[i][0] = *reinterpret_cast<const f32x4 *>(from + (c + i) * step);
+                v[i][1] = *reinterpret_cast<const f32x4 *>(from + (c + i) * step + 4);
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f.v[e] += v[i][0][e], f.v[4 + e] += v[i][1][e];
+    }
+    if (is_bias) write8(make_rsrc(g.d_bias + (int64_t)group * g.N, kRecords), (uint32_t)at, true, f);
+    else write8(make_rsrc(g.out + (group * g.out_group + at) * (g.out32 ? 4 : 2), kRecords), 0, g.out32, f);
 }
 
 template <Job JOB, int WI, int WJ, int MI, int NJ, int SA, int SB, int KB>
@@ -737,8 +908,9 @@ int launch_shape(const GemmArgs &g, hipStream_t st)
     const int e = allow_lds(grant, kernel, Sh::kLds);
     if (e) return e;
     int64_t tiles;                                            // at most
-    if (JOB == Job::weights) {
-        tiles = (int64_t)g.groups * ((g.N + Sh::BM - 1) / Sh::BM) * ((g.K + Sh::BN - 1) / Sh::BN);
+    if (Sh::kAcrossA) {
+        const int64_t matrices = JOB == Job::parts ? g.M / g.chunk + (g.groups < g.M ? g.groups : g.M) : g.groups;
+        tiles = matrices * ((g.N + Sh::BM - 1) / Sh::BM) * ((g.K + Sh::BN - 1) / Sh::BN);
     } else {
         const int cols = JOB == Job::product ? g.N : g.K;
         tiles = (int64_t)(g.M / Sh::BM + (g.groups < g.M ? g.groups : g.M)) * ((cols + Sh::BN - 1) / Sh::BN);
@@ -746,6 +918,34 @@ int launch_shape(const GemmArgs &g, hipStream_t st)
     const int64_t most = Sh::kPerUnit * stream_compute_units(st), grid = tiles < most ? (tiles + 7) / 8 * 8 : most;
     expert_gemm_tiles<JOB, WI, WJ, MI, NJ, SA, SB, KB><<<(uint32_t)grid, Sh::kThreads, Sh::kLds, st>>>(g);
     return (int)hipGetLastError();
+}
+
+template <Job JOB>
+int launch_few(const GemmArgs &g, hipStream_t st)
+{
+    static LdsGrant grant;
+    constexpr int kBytes = kFewWaves * kFewStages * 8192;
+    const int e = allow_lds(grant, (const void *)expert_gemm_few<JOB>, kBytes);
+    if (e) return e;
+    const int cols = JOB == Job::product ? g.N : g.K;
+    const int64_t tiles = (int64_t)(g.M / 32 + (g.groups < g.M ? g.groups : g.M)) * ((cols + 31) / 32);
+    expert_gemm_few<JOB><<<(uint32_t)((tiles + 7) / 8 * 8), kFewWaves * 64, kBytes, st>>>(g);
+    return (int)hipGetLastError();
+}
+
+// Rows through experts, forward or back, by the shape that the rule picks.
+template <Job JOB>
+int launch_rows_job(const GemmArgs &g, hipStream_t st)
+{
+    const int cols = JOB == Job::product ? g.N : g.K, length = JOB == Job::product ? g.K : g.N;
+    switch (expert_tiles(g.M, g.groups, cols, length)) {
+    case ExpertTiles::few: return launch_few<JOB>(g, st);
+    case ExpertTiles::rows32: return launch_shape<JOB, 1, 4, 1, 1, 4, 4, 64>(g, st);
+    case ExpertTiles::rows64: return launch_shape<JOB, 1, 4, 2, 2, 2, 2, 64>(g, st);
+    case ExpertTiles::square128: return launch_shape<JOB, 2, 2, 2, 2, 2, 3, 64>(g, st);
+    case ExpertTiles::rows256: break;
+    }
+    return launch_shape<JOB, 2, 4, 4, 2, 2, 3, 64>(g, st);
 }
 
 GemmArgs args_of(const ExpertGemmShape &s, const int32_t *offsets, int32_t M)
@@ -764,7 +964,7 @@ int launch_expert_gemm(const ExpertGemmShape &s, const void *x, int64_t ldx, int
     g.a = (const char *)x, g.lda = ldx, g.b = (const char *)w, g.ldb = s.K, g.b_group = (int64_t)s.N * s.K;
     g.bias = bias, g.pre = (char *)pre, g.ld_pre = ld_pre, g.residual = (const char *)residual, g.ld_res = ld_res;
     g.out = (char *)y, g.ldo = ldy;
-    return launch_shape<Job::product, 2, 4, 4, 2, 2, 3, 64>(g, st);
+    return launch_rows_job<Job::product>(g, st);
 }
 
 int launch_expert_gemm_input(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, int32_t M, const void *w, const int32_t *offsets, const void *pre,
@@ -774,16 +974,28 @@ int launch_expert_gemm_input(const ExpertGemmShape &s, const void *dy, int64_t l
     g.a = (const char *)dy, g.lda = ld_dy, g.b = (const char *)w, g.ldb = s.K, g.b_group = (int64_t)s.N * s.K;
     g.pre = (char *)const_cast<void *>(pre), g.ld_pre = ld_pre;
     g.out = (char *)dx, g.ldo = ld_dx;
-    return launch_shape<Job::input, 2, 4, 4, 2, 2, 3, 64>(g, st);
+    return launch_rows_job<Job::input>(g, st);
 }
 
 int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, int32_t M, const int32_t *offsets,
-                               void *dw, float *d_bias, void *, hipStream_t st)
+                               void *dw, float *d_bias, void *ws, hipStream_t st)
 {
     GemmArgs g = args_of(s, offsets, M);
     g.a = (const char *)dy, g.lda = ld_dy, g.b = (const char *)x, g.ldb = ldx;
     g.out = (char *)dw, g.ldo = s.K, g.out_group = (int64_t)s.N * s.K, g.d_bias = d_bias;
-    return launch_shape<Job::weights, 2, 4, 4, 2, 2, 3, 64>(g, st);
+    g.chunk = expert_weights_chunk(M, s.groups, s.N, s.K);
+    if (g.chunk == 0) {
+        if (expert_weights_small(s.groups, s.N, s.K)) return launch_shape<Job::weights, 2, 2, 2, 2, 2, 3, 64>(g, st);
+        return launch_shape<Job::weights, 2, 4, 4, 2, 2, 3, 64>(g, st);
+    }
+    GemmArgs p = g;                                           // the parts, in fp32, behind one another; then their sums of dy
+    p.out = (char *)ws, p.out32 = 1;
+    p.d_bias = d_bias ? (float *)ws + expert_weights_parts(M, s.groups, g.chunk) * s.N * s.K : nullptr;
+    const int e = launch_shape<Job::parts, 2, 2, 2, 2, 2, 3, 64>(p, st);
+    if (e) return e;
+    const int64_t pieces = (int64_t)s.N * s.K / 8 + (d_bias ? s.N / 8 : 0);
+    expert_weights_add<<<(uint32_t)(s.groups * ((pieces + kAddThreads - 1) / kAddThreads)), kAddThreads, 0, st>>>(g, (const float *)ws, p.d_bias);
+    return (int)hipGetLastError();
 }
 
 }  // namespace sida
