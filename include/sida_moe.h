@@ -490,7 +490,7 @@ int sida_route_backward(const sida_route_config *cfg, const void *logits_dev, in
  * (below) and sum; and the way back.  No context is needed; the calls are asynchronous on `stream`, allocate nothing and may be captured into a HIP graph.
  * Pair p = t * top_k + j is token t's j-th expert.  It takes part where its id lies within [0,E) and its gate (where gates are given) is not 0: a
  * router's gates are 0 where a token is masked, and a caller without one gives ids of -1.
- * T tokens, E <= SIDA_MAX_E, top_k <= SIDA_MAX_TOP_K, T * top_k < 2^31. */
+ * T tokens, E <= SIDA_MAX_E, top_k <= SIDA_MAX_TOP_K, T * top_k < 2^26. */
 
 /* Sorts the pairs by expert, those of one expert in their order:
  *     offsets_dev int32 [E+1]      exclusive sums of the pairs per expert; offsets[E] is how many take part

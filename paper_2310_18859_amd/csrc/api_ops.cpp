@@ -37,7 +37,8 @@ RouteShape route_shape(const sida_route_config *c) { return RouteShape{c->E, c->
 
 bool pairs_ok(int32_t E, int32_t top_k, int32_t T)
 {
-    return E >= 1 && E <= SIDA_MAX_E && top_k >= 1 && top_k <= SIDA_MAX_TOP_K && T >= 0 && (int64_t)T * top_k <= INT32_MAX;
+    return E >= 1 && E <= SIDA_MAX_E && top_k >= 1 && top_k <= SIDA_MAX_TOP_K && T >= 0 &&
+           (int64_t)T * top_k < 1 << 26;                      // 64 lanes each: a launch has fewer than 2^32
 }
 bool rows_cfg_ok(const sida_expert_rows_config *c)
 {

@@ -605,24 +605,25 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         };
-        if (whole > 0) fetch(0, 0);
-#pragma clang loop unroll(disable)
-        for (int t = 0; t < stages; ++t) {
-            if (t < whole) {
-#pragma unroll
-                for (int q = 0; q < Q - 1; ++q) {
-                    fetch(q + 1, q + 1 & 1);
-#pragma unroll
-                    for (int m = 0; m < MB; ++m) block(q, m);
-                    add_bias(q);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                add_bias(Q - 1);
-            }
+        auto go_on = [&] {                                    // to the next stage
             slot_a = slot_a == SA - 1 ? 0 : slot_a + 1;
             slot_b = slot_b == SB - 1 ? 0 : slot_b + 1;
             prepare();
             arrived();
+        };
+        if (whole > 0) fetch(0, 0);
+#pragma clang loop unroll(disable)
+        for (int t = 0; t < whole; ++t) {
+#pragma unroll
+            for (int q = 0; q < Q - 1; ++q) {
+                fetch(q + 1, q + 1 & 1);
+#pragma unroll
+                for (int m = 0; m < MB; ++m) block(q, m);
+                add_bias(q);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            add_bias(Q - 1);
+            go_on();
             if (t + 1 < whole) fetch(0, 0);                   // the next tile's first are read when it begins
             // The loads of the stage that takes this one's place, between the products of its last step.
             constexpr int kEach = (kLoads + MR - 1) / MR;
@@ -630,9 +631,15 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
             for (int m = 0; m < MR; ++m) {
 #pragma unroll
                 for (int i = m * kEach; i < (m + 1) * kEach && i < kLoads; ++i) load(i);
-                if (MB > 0 && t < whole) block(Q - 1, m);
+                if (MB > 0) block(Q - 1, m);
                 __builtin_amdgcn_sched_barrier(0);
             }
+        }
+#pragma clang loop unroll(disable)
+        for (int t = whole; t < stages; ++t) {                // stages that hold nothing: sums shorter than the ring (a check in the loop above costs 2 to 6%)
+            go_on();
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load(i);
         }
 
         // ---- results.  A lane holds four times four consecutive columns of one row of a block, lane ^ 32 the four beside them.  Two exchanges, between

@@ -144,6 +144,8 @@ __global__ __launch_bounds__(kSortThreads) void expert_sort_place(const SortArgs
 }
 
 // ---- rows ---------------------------------------------------------------------------------------
+// Bound by bytes where there are many tokens, and by the way to memory and back where there are few: what a token's pairs read is asked for together,
+// KM pairs and kDepth pieces of a row at a time.
 struct RowsArgs {
     const int32_t *places;
     const float *gates;          // may be NULL: ones
@@ -153,164 +155,206 @@ struct RowsArgs {
     void *to_rows, *y;
     float *d_gates;              // may be NULL
     int64_t ld_x, ld_rows, ld_res, ld_to_rows, ld_y;   // values between rows
-    int T, M, k, pieces;         // expert rows there are, pieces of a row
-    int lanes_log2;              // lanes of a token
+    int T, M, k, d;              // expert rows there are, values of a row
+    int lanes_log2;              // lanes of a token, or of a pair
 };
 
-constexpr int kRowsThreads = 256;
+constexpr int kRowsThreads = 256, kDepth = 2;
 
-// A piece of a row: BYTES of values of type V.
-template <class V, int BYTES>
+// A piece of a row: BYTES of values of type V, at any address of ALIGN bytes.
+template <class V, int BYTES, int ALIGN>
 struct Piece {
     static constexpr int kOf = BYTES / (int)sizeof(V);
     typedef __attribute__((ext_vector_type(kOf))) V Vec;
+    typedef Vec __attribute__((aligned(ALIGN))) Any;
+    static __device__ __forceinline__ Vec get(const V *p) { return *reinterpret_cast<const Any *>(p); }
+    static __device__ __forceinline__ void put(V *p, Vec v)
+    {
+        if constexpr (ALIGN == 16) __builtin_nontemporal_store(v, reinterpret_cast<Vec *>(p));   // whole lines, past L2's replacement
+        else *reinterpret_cast<Any *>(p) = v;
+    }
+    static __device__ __forceinline__ float at(const Vec &v, int i) { return (float)v[i]; }
+    static __device__ __forceinline__ void set(Vec &v, int i, float f) { v[i] = (V)f; }
 };
-template <class V>
-struct Piece<V, (int)sizeof(V)> {
+template <class V, int ALIGN>
+struct Piece<V, (int)sizeof(V), ALIGN> {
     static constexpr int kOf = 1;
     typedef V Vec;
+    static __device__ __forceinline__ V get(const V *p) { return *p; }
+    static __device__ __forceinline__ void put(V *p, V v) { *p = v; }
+    static __device__ __forceinline__ float at(V v, int) { return (float)v; }
+    static __device__ __forceinline__ void set(V &v, int, float f) { v = (V)f; }
 };
-template <class V, int BYTES>
-__device__ __forceinline__ void widen(const typename Piece<V, BYTES>::Vec &v, float *f)
-{
-    if constexpr (Piece<V, BYTES>::kOf == 1) {
-        f[0] = (float)v;
-    } else {
-#pragma unroll
-        for (int i = 0; i < Piece<V, BYTES>::kOf; ++i) f[i] = (float)v[i];
-    }
-}
-template <class V, int BYTES>
-__device__ __forceinline__ typename Piece<V, BYTES>::Vec narrow(const float *f)
-{
-    typename Piece<V, BYTES>::Vec v;
-    if constexpr (Piece<V, BYTES>::kOf == 1) {
-        v = (V)f[0];
-    } else {
-#pragma unroll
-        for (int i = 0; i < Piece<V, BYTES>::kOf; ++i) v[i] = (V)f[i];
-    }
-    return v;
-}
-template <class Vec>
-__device__ __forceinline__ void put(Vec v, Vec *to)
-{
-    if constexpr (sizeof(Vec) == 16) __builtin_nontemporal_store(v, to);
-    else *to = v;
-}
 
-// Lanes of a token: `sub` of 2^lanes_log2, so that short rows share a wavefront.
-struct Token {
+// Lanes of a token (or pair): `sub` of 2^lanes_log2, so that short rows share a wavefront.
+struct Lanes {
     int64_t t;
     int sub, lanes;
 };
-__device__ __forceinline__ Token token_of(const RowsArgs &a)
+__device__ __forceinline__ Lanes lanes_of(const RowsArgs &a)
 {
     const int64_t at = (int64_t)blockIdx.x * kRowsThreads + threadIdx.x;
-    return Token{at >> a.lanes_log2, (int)at & (1 << a.lanes_log2) - 1, 1 << a.lanes_log2};
+    return Lanes{at >> a.lanes_log2, (int)at & ((1 << a.lanes_log2) - 1), 1 << a.lanes_log2};
 }
-// A token's place for its j-th expert; -1 also for one past the rows there are.
-__device__ __forceinline__ int place_of(const RowsArgs &a, int64_t t, int j)
+// A place; -1 also for one past the rows there are.
+__device__ __forceinline__ int place_at(const RowsArgs &a, int64_t p)
 {
-    const int at = a.places[t * a.k + j];
+    const int at = a.places[p];
     return (uint32_t)at < (uint32_t)a.M ? at : -1;
 }
+// The pieces of a row: of 16 bytes, and what is left of it in the smallest pieces that its alignment allows.
+template <class V, int ALIGN, class Use>
+__device__ __forceinline__ void each_piece(int d, Use &&use)
+{
+    constexpr int kOf = 16 / (int)sizeof(V);
+    if constexpr (ALIGN >= 4) {
+        use(Piece<V, 16, ALIGN>(), 0, d / kOf);
+        if constexpr (ALIGN < 16) use(Piece<V, 4, 4>(), d / kOf * kOf, d % kOf / (4 / (int)sizeof(V)));
+    } else {
+        use(Piece<V, (int)sizeof(V), ALIGN>(), 0, d);
+    }
+}
 
-template <class V, int BYTES>
+template <class V, int ALIGN, int KM>
 __global__ __launch_bounds__(kRowsThreads) void expert_rows_out(const RowsArgs a)
 {
-    typedef Piece<V, BYTES> P;
-    const Token me = token_of(a);
+    const Lanes me = lanes_of(a);
     if (me.t >= a.T) return;
     const V *x = (const V *)a.x + me.t * a.ld_x;
-    for (int i = me.sub; i < a.pieces; i += me.lanes) {
-        const typename P::Vec v = *reinterpret_cast<const typename P::Vec *>(x + i * P::kOf);
-        for (int j = 0; j < a.k; ++j) {
-            const int at = place_of(a, me.t, j);
-            if (at >= 0) put(v, reinterpret_cast<typename P::Vec *>((V *)a.to_rows + (int64_t)at * a.ld_to_rows + i * P::kOf));
-        }
+    V *to[KM];
+#pragma unroll
+    for (int j = 0; j < KM; ++j) {
+        const int at = j < a.k ? place_at(a, me.t * a.k + j) : -1;
+        to[j] = at >= 0 ? (V *)a.to_rows + (int64_t)at * a.ld_to_rows : nullptr;
     }
+    each_piece<V, ALIGN>(a.d, [&](auto piece, int from, int pieces) {
+        typedef decltype(piece) P;
+        for (int i0 = me.sub; i0 < pieces; i0 += me.lanes * kDepth) {
+            typename P::Vec v[kDepth];
+#pragma unroll
+            for (int u = 0; u < kDepth; ++u) {
+                const int i = i0 + u * me.lanes;
+                v[u] = P::get(x + from + (i < pieces ? i : i0) * P::kOf);
+            }
+#pragma unroll
+            for (int u = 0; u < kDepth; ++u)
+                if (i0 + u * me.lanes < pieces)
+#pragma unroll
+                    for (int j = 0; j < KM; ++j)
+                        if (to[j]) P::put(to[j] + from + (i0 + u * me.lanes) * P::kOf, v[u]);
+        }
+    });
 }
 
-template <class V, int BYTES>
+template <class V, int ALIGN, int KM>
 __global__ __launch_bounds__(kRowsThreads) void expert_rows_sum(const RowsArgs a)
 {
-    typedef Piece<V, BYTES> P;
-    const Token me = token_of(a);
+    const Lanes me = lanes_of(a);
     if (me.t >= a.T) return;
-    for (int i = me.sub; i < a.pieces; i += me.lanes) {
-        float sum[P::kOf] = {};
-        for (int j = 0; j < a.k; ++j) {
-            const int at = place_of(a, me.t, j);
-            if (at < 0) continue;
-            const float gate = a.gates ? a.gates[me.t * a.k + j] : 1.f;
-            float f[P::kOf];
-            widen<V, BYTES>(*reinterpret_cast<const typename P::Vec *>((const V *)a.rows + (int64_t)at * a.ld_rows + i * P::kOf), f);
+    // A pair without a part reads the first value's place (if there are rows at all) and counts for nothing.
+    const V *from_row[KM];
+    float gate[KM];
+    bool part[KM];
 #pragma unroll
-            for (int q = 0; q < P::kOf; ++q) sum[q] += gate * f[q];
-        }
-        if (a.residual) {
-            float f[P::kOf];
-            widen<V, BYTES>(*reinterpret_cast<const typename P::Vec *>((const V *)a.residual + me.t * a.ld_res + i * P::kOf), f);
-#pragma unroll
-            for (int q = 0; q < P::kOf; ++q) sum[q] += f[q];
-        }
-        put(narrow<V, BYTES>(sum), reinterpret_cast<typename P::Vec *>((V *)a.y + me.t * a.ld_y + i * P::kOf));
+    for (int j = 0; j < KM; ++j) {
+        const int at = j < a.k ? place_at(a, me.t * a.k + j) : -1;
+        part[j] = at >= 0;
+        from_row[j] = (const V *)a.rows + (int64_t)max(at, 0) * a.ld_rows;
+        gate[j] = a.gates && part[j] ? a.gates[me.t * a.k + j] : 1.f;
     }
+    each_piece<V, ALIGN>(a.d, [&](auto piece, int from, int pieces) {
+        typedef decltype(piece) P;
+        for (int i = me.sub; i < pieces; i += me.lanes) {
+            const int at = from + i * P::kOf;
+            typename P::Vec v[KM], res{};
+#pragma unroll
+            for (int j = 0; j < KM; ++j)
+                if (part[j]) v[j] = P::get(from_row[j] + at);
+            if (a.residual) res = P::get((const V *)a.residual + me.t * a.ld_res + at);
+            float sum[P::kOf] = {};
+#pragma unroll
+            for (int j = 0; j < KM; ++j)
+                if (part[j])
+#pragma unroll
+                    for (int q = 0; q < P::kOf; ++q) sum[q] += gate[j] * P::at(v[j], q);
+            typename P::Vec out;
+#pragma unroll
+            for (int q = 0; q < P::kOf; ++q) P::set(out, q, a.residual ? sum[q] + P::at(res, q) : sum[q]);
+            P::put((V *)a.y + me.t * a.ld_y + at, out);
+        }
+    });
 }
 
-template <class V, int BYTES>
+// A pair to a group of lanes (with a token to it its pairs would wait for one another).
+template <class V, int ALIGN>
 __global__ __launch_bounds__(kRowsThreads) void expert_rows_back(const RowsArgs a)
 {
-    typedef Piece<V, BYTES> P;
-    const Token me = token_of(a);
-    if (me.t >= a.T) return;
-    const V *dy = (const V *)a.x + me.t * a.ld_x;
-    for (int j = 0; j < a.k; ++j) {
-        const int at = place_of(a, me.t, j);
-        float dot = 0;
-        if (at >= 0) {
-            const float gate = a.gates ? a.gates[me.t * a.k + j] : 1.f;
-            for (int i = me.sub; i < a.pieces; i += me.lanes) {
-                float f[P::kOf], g[P::kOf];
-                widen<V, BYTES>(*reinterpret_cast<const typename P::Vec *>(dy + i * P::kOf), f);
-                if (a.d_gates) {
-                    widen<V, BYTES>(*reinterpret_cast<const typename P::Vec *>((const V *)a.rows + (int64_t)at * a.ld_rows + i * P::kOf), g);
+    const Lanes me = lanes_of(a);
+    if (me.t >= (int64_t)a.T * a.k) return;
+    const int at = place_at(a, me.t);
+    float dot = 0;
+    if (at >= 0) {
+        const float gate = a.gates ? a.gates[me.t] : 1.f;
+        const V *dy = (const V *)a.x + me.t / a.k * a.ld_x, *row = (const V *)a.rows + (int64_t)at * a.ld_rows;
+        V *to = (V *)a.to_rows + (int64_t)at * a.ld_to_rows;
+        each_piece<V, ALIGN>(a.d, [&](auto piece, int from, int pieces) {
+            typedef decltype(piece) P;
+            for (int i0 = me.sub; i0 < pieces; i0 += me.lanes * kDepth) {
+                typename P::Vec g[kDepth], r[kDepth];
 #pragma unroll
-                    for (int q = 0; q < P::kOf; ++q) dot += f[q] * g[q];
+                for (int u = 0; u < kDepth; ++u) {
+                    const int i = i0 + u * me.lanes, value = from + (i < pieces ? i : i0) * P::kOf;
+                    g[u] = P::get(dy + value);
+                    if (a.d_gates) r[u] = P::get(row + value);
                 }
 #pragma unroll
-                for (int q = 0; q < P::kOf; ++q) f[q] *= gate;
-                put(narrow<V, BYTES>(f), reinterpret_cast<typename P::Vec *>((V *)a.to_rows + (int64_t)at * a.ld_to_rows + i * P::kOf));
+                for (int u = 0; u < kDepth; ++u) {
+                    const int i = i0 + u * me.lanes;
+                    if (i >= pieces) break;
+                    typename P::Vec out;
+#pragma unroll
+                    for (int q = 0; q < P::kOf; ++q) {
+                        const float f = P::at(g[u], q);
+                        if (a.d_gates) dot += f * P::at(r[u], q);
+                        P::set(out, q, gate * f);
+                    }
+                    P::put(to + from + i * P::kOf, out);
+                }
             }
-        }
-        if (a.d_gates) {
-            for (int d = 1; d < me.lanes; d *= 2) dot += __shfl_xor(dot, d);
-            if (me.sub == 0) a.d_gates[me.t * a.k + j] = dot;
-        }
+        });
+    }
+    if (a.d_gates) {
+        for (int d = 1; d < me.lanes; d *= 2) dot += __shfl_xor(dot, d);
+        if (me.sub == 0) a.d_gates[me.t] = dot;
     }
 }
 
 enum class RowsWay { out, sum, back };
-template <class V, int BYTES>
-int launch_way(RowsArgs &a, RowsWay way, int32_t d, hipStream_t st)
+template <class V, int ALIGN>
+int launch_way(RowsArgs &a, RowsWay way, hipStream_t st)
 {
-    a.pieces = d / (BYTES / (int)sizeof(V));
-    a.lanes_log2 = rows_lanes_log2(a.pieces);
-    const uint32_t grid = (uint32_t)(((int64_t)a.T * (1 << a.lanes_log2) + kRowsThreads - 1) / kRowsThreads);
+    a.lanes_log2 = rows_lanes_log2(ALIGN >= 4 ? a.d * (int)sizeof(V) / 16 : a.d);
+    const int64_t of = way == RowsWay::back ? (int64_t)a.T * a.k : a.T;
+    const uint32_t grid = (uint32_t)(((of << a.lanes_log2) + kRowsThreads - 1) / kRowsThreads);
+    auto by_pairs = [&](auto one, auto two, auto four, auto eight) {
+        if (a.k == 1) one<<<grid, kRowsThreads, 0, st>>>(a);
+        else if (a.k == 2) two<<<grid, kRowsThreads, 0, st>>>(a);
+        else if (a.k <= 4) four<<<grid, kRowsThreads, 0, st>>>(a);
+        else eight<<<grid, kRowsThreads, 0, st>>>(a);
+    };
     switch (way) {
-    case RowsWay::out: expert_rows_out<V, BYTES><<<grid, kRowsThreads, 0, st>>>(a); break;
-    case RowsWay::sum: expert_rows_sum<V, BYTES><<<grid, kRowsThreads, 0, st>>>(a); break;
-    case RowsWay::back: expert_rows_back<V, BYTES><<<grid, kRowsThreads, 0, st>>>(a); break;
+    case RowsWay::out: by_pairs(expert_rows_out<V, ALIGN, 1>, expert_rows_out<V, ALIGN, 2>, expert_rows_out<V, ALIGN, 4>, expert_rows_out<V, ALIGN, 8>); break;
+    case RowsWay::sum: by_pairs(expert_rows_sum<V, ALIGN, 1>, expert_rows_sum<V, ALIGN, 2>, expert_rows_sum<V, ALIGN, 4>, expert_rows_sum<V, ALIGN, 8>); break;
+    case RowsWay::back: expert_rows_back<V, ALIGN><<<grid, kRowsThreads, 0, st>>>(a); break;
     }
     return (int)hipGetLastError();
 }
-// Pieces of 16 bytes where all rows start and end on such boundaries, else 4, else single values.
-int launch_rows(RowsArgs &a, RowsWay way, bool fp32, int32_t d, size_t ends, hipStream_t st)
+// By the alignment of all rows' beginnings and ends: 16 bytes, 4, or single bf16 values.
+int launch_rows(RowsArgs &a, RowsWay way, bool fp32, size_t ends, hipStream_t st)
 {
-    if (fp32) return ends % 16 == 0 ? launch_way<float, 16>(a, way, d, st) : launch_way<float, 4>(a, way, d, st);
-    if (ends % 16 == 0) return launch_way<__bf16, 16>(a, way, d, st);
-    return ends % 4 == 0 ? launch_way<__bf16, 4>(a, way, d, st) : launch_way<__bf16, 2>(a, way, d, st);
+    if (fp32) return ends % 16 == 0 ? launch_way<float, 16>(a, way, st) : launch_way<float, 4>(a, way, st);
+    if (ends % 16 == 0) return launch_way<__bf16, 16>(a, way, st);
+    return ends % 4 == 0 ? launch_way<__bf16, 4>(a, way, st) : launch_way<__bf16, 2>(a, way, st);
 }
 size_t ends_of(const void *p, int64_t ld, size_t size) { return (size_t)(uintptr_t)p | (size_t)ld * size; }
 
@@ -337,9 +381,9 @@ int launch_expert_sort(const int32_t *ids, const float *gates, int64_t pairs, in
 int launch_expert_rows(const ExpertRowsShape &s, const void *x, int64_t ld_x, const int32_t *places, void *rows, int64_t ld_rows, hipStream_t st)
 {
     RowsArgs a{};
-    a.places = places, a.x = x, a.to_rows = rows, a.ld_x = ld_x, a.ld_to_rows = ld_rows, a.T = s.T, a.M = s.M, a.k = s.k;
+    a.places = places, a.x = x, a.to_rows = rows, a.ld_x = ld_x, a.ld_to_rows = ld_rows, a.T = s.T, a.M = s.M, a.k = s.k, a.d = s.d;
     const size_t size = s.fp32 ? 4 : 2;
-    return launch_rows(a, RowsWay::out, s.fp32, s.d, ends_of(x, ld_x, size) | ends_of(rows, ld_rows, size) | s.d * size, st);
+    return launch_rows(a, RowsWay::out, s.fp32, ends_of(x, ld_x, size) | ends_of(rows, ld_rows, size) | s.d * size, st);
 }
 
 int launch_expert_sum(const ExpertRowsShape &s, const void *rows, int64_t ld_rows, const int32_t *places, const float *gates, const void *residual,
@@ -347,9 +391,9 @@ int launch_expert_sum(const ExpertRowsShape &s, const void *rows, int64_t ld_row
 {
     RowsArgs a{};
     a.places = places, a.gates = gates, a.rows = rows, a.residual = residual, a.y = y, a.ld_rows = ld_rows, a.ld_res = ld_res, a.ld_y = ld_y;
-    a.T = s.T, a.M = s.M, a.k = s.k;
+    a.T = s.T, a.M = s.M, a.k = s.k, a.d = s.d;
     const size_t size = s.fp32 ? 4 : 2;
-    return launch_rows(a, RowsWay::sum, s.fp32, s.d,
+    return launch_rows(a, RowsWay::sum, s.fp32,
                        ends_of(rows, ld_rows, size) | ends_of(y, ld_y, size) | (residual ? ends_of(residual, ld_res, size) : 0) | s.d * size, st);
 }
 
@@ -358,9 +402,9 @@ int launch_expert_sum_backward(const ExpertRowsShape &s, const void *dy, int64_t
 {
     RowsArgs a{};
     a.places = places, a.gates = gates, a.x = dy, a.rows = rows, a.to_rows = d_rows, a.d_gates = d_gates;
-    a.ld_x = ld_dy, a.ld_rows = ld_rows, a.ld_to_rows = ld_d, a.T = s.T, a.M = s.M, a.k = s.k;
+    a.ld_x = ld_dy, a.ld_rows = ld_rows, a.ld_to_rows = ld_d, a.T = s.T, a.M = s.M, a.k = s.k, a.d = s.d;
     const size_t size = s.fp32 ? 4 : 2;
-    return launch_rows(a, RowsWay::back, s.fp32, s.d,
+    return launch_rows(a, RowsWay::back, s.fp32,
                        ends_of(dy, ld_dy, size) | ends_of(d_rows, ld_d, size) | (d_gates ? ends_of(rows, ld_rows, size) : 0) | s.d * size, st);
 }
 

@@ -14,18 +14,18 @@ def sort(E=8, k=2, ids=P, gates=0, T=5, offsets=P, places=P, ws=P, n=1 << 20):
     return sm.lib().sida_expert_sort(E, k, ids, gates, T, offsets, places, ws, n, 0)
 
 
-@pytest.mark.parametrize("bad", [dict(E=0), dict(E=257), dict(k=0), dict(k=9), dict(T=-1), dict(T=1 << 30), dict(ids=0), dict(offsets=0), dict(places=0), dict(ws=0),
+@pytest.mark.parametrize("bad", [dict(E=0), dict(E=257), dict(k=0), dict(k=9), dict(T=-1), dict(T=1 << 25), dict(ids=0), dict(offsets=0), dict(places=0), dict(ws=0),
                                  dict(ids=P + 2), dict(gates=P + 1), dict(offsets=P + 2), dict(places=P + 1), dict(ws=P + 2)])
 def test_sort_refuses(bad):
     assert sort(**bad) == EINVAL
 
 
 def test_sort_workspace():
-    for T, chunks in ((0, 1), (1, 1), (2048, 1), (2049, 3), (1 << 18, 256), ((1 << 30) - 1, 256)):
+    for T, chunks in ((0, 1), (1, 1), (2048, 1), (2049, 3), (1 << 18, 256), ((1 << 25) - 1, 256)):
         n = sm.expert_sort_workspace_bytes(64, 2, T)
         assert n == chunks * 256
         assert sort(E=64, T=T, n=n - 1) == ENOSPC
-    for bad in ((0, 1, 5), (257, 1, 5), (8, 9, 5), (8, 1, -1), (8, 2, 1 << 30), (8, 1, 1 << 40), (1 << 33, 1, 5)):
+    for bad in ((0, 1, 5), (257, 1, 5), (8, 9, 5), (8, 1, -1), (8, 2, 1 << 25), (8, 1, 1 << 40), (1 << 33, 1, 5)):
         assert sm.expert_sort_workspace_bytes(*bad) == 0
 
 
@@ -45,7 +45,7 @@ def back(dy=P, ld_dy=64, rows=P, ld_rows=64, places=P, gates=0, d_rows=P, ld_d=6
     return sm.lib().sida_expert_sum_backward(cfg_rows(**c), dy, ld_dy, rows, ld_rows, places, gates, d_rows, ld_d, dg, 0)
 
 
-CFG = [dict(cfg=False), dict(T=-1), dict(k=0), dict(k=9), dict(T=1 << 30), dict(M=-1), dict(d=0), dict(d=65537), dict(kind=sm.MXFP4), dict(kind=-1), dict(places=0),
+CFG = [dict(cfg=False), dict(T=-1), dict(k=0), dict(k=9), dict(T=1 << 25), dict(M=-1), dict(d=0), dict(d=65537), dict(kind=sm.MXFP4), dict(kind=-1), dict(places=0),
        dict(places=P + 2)]
 
 
