@@ -496,7 +496,7 @@ int sida_route_backward(const sida_route_config *cfg, const void *logits_dev, in
  *     offsets_dev int32 [E+1]      exclusive sums of the pairs per expert; offsets[E] is how many take part
  *     places_dev  int32 [T,top_k]  the pair's row in expert order, -1 without a part
  * ids_dev int32 [T,top_k]; gates_dev NULL or fp32 [T,top_k] (0 and -0: no part; NaN takes part); workspace_dev 4-byte aligned,
- * >= sida_expert_sort_workspace_bytes(E, top_k, T), scratch of this call alone until it is done. */
+ * >= sida_expert_sort_workspace_bytes(E, top_k, T) (enough for fewer tokens, too), scratch of this call alone until it is done. */
 size_t sida_expert_sort_workspace_bytes(int32_t E, int32_t top_k, int32_t T);  /* 0 on bad arguments */
 int sida_expert_sort(int32_t E, int32_t top_k, const int32_t *ids_dev, const float *gates_dev, int32_t T, int32_t *offsets_dev,
                      int32_t *places_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
@@ -533,7 +533,8 @@ int sida_expert_sum_backward(const sida_expert_rows_config *cfg, const void *dy_
  *   offsets_dev int32 [groups+1], ascending, 0 .. M (values outside are taken as the nearest of 0 and M, a group whose end is before its start as empty;
  *               with offsets that do not ascend, which rows are computed is not defined; no others are touched).  Rows of no group
  *               keep what they hold, and are not read.  NULL with one group: all rows.
- * Limits: 1 <= groups <= SIDA_MAX_E; N, K in 8 .. 65536, N * K <= 2^30, groups * N * K <= 2^36; 0 <= M <= 2^24; M * N and M * K <= 2^35; rows at most 2^22 values apart. */
+ * Limits: 1 <= groups <= SIDA_MAX_E; N, K in 8 .. 65536, N * K <= 2^30, groups * N * K <= 2^36; 0 <= M <= 2^24; M * N and M * K <= 2^35; rows at most 2^23 bytes
+ * apart. */
 enum { SIDA_ACT_NONE = 0, SIDA_ACT_RELU = 1, SIDA_ACT_GELU = 2, SIDA_ACT_SILU = 3 };
 typedef struct sida_expert_gemm_config {
     int32_t groups;       /* experts                                            */
@@ -555,8 +556,9 @@ int sida_expert_gemm(const sida_expert_gemm_config *cfg, const void *x_dev, int6
 int sida_expert_gemm_input(const sida_expert_gemm_config *cfg, const void *dy_dev, int64_t ld_dy, int32_t M, const void *w_dev,
                            const int32_t *offsets_dev, const void *pre_dev, int64_t ld_pre, void *dx_dev, int64_t ld_dx, void *stream);
 /* The gradients of matrices and biases:  dW_g = sum_r dy[r] x[r]^T,  dbias_g = sum_r dy[r]  over the rows r of group g; 0 for a group without rows.
- *   dy_dev bf16 [M, N], x_dev bf16 [M, K], dw_dev out_type [groups, N, K], d_bias_dev NULL or fp32 [groups, N]
- *   workspace_dev  16-byte aligned, >= sida_expert_gemm_weights_workspace_bytes(cfg, M), scratch of this call alone until it is done (NULL where that is 0) */
+ *   dy_dev bf16 [M, N], x_dev bf16 [M, K], dw_dev out_type [groups, N, K], d_bias_dev NULL or fp32 [groups, N] (16-byte aligned)
+ *   workspace_dev  16-byte aligned, >= sida_expert_gemm_weights_workspace_bytes(cfg, M) (enough for fewer rows, too), scratch of this call alone until
+ *                  it is done (NULL where that is 0) */
 size_t sida_expert_gemm_weights_workspace_bytes(const sida_expert_gemm_config *cfg, int32_t M);
 int sida_expert_gemm_weights(const sida_expert_gemm_config *cfg, const void *dy_dev, int64_t ld_dy, const void *x_dev, int64_t ldx, int32_t M,
                              const int32_t *offsets_dev, void *dw_dev, float *d_bias_dev, void *workspace_dev, size_t workspace_bytes, void *stream);

@@ -57,7 +57,8 @@ bool expert_cfg_ok(const sida_expert_gemm_config *c, int32_t M)
 }
 bool matrix_ok(const void *p, int64_t ld, int32_t cols, int32_t type)
 {
-    return p && aligned(p, 16) && ld >= cols && ld <= kMostExpertPitch && ld % (type == SIDA_FP32 ? 4 : 8) == 0;
+    return p && aligned(p, 16) && ld >= cols && ld < kMostPitch && ld * (type == SIDA_FP32 ? 4 : 2) <= kMostExpertPitch &&
+           ld % (type == SIDA_FP32 ? 4 : 8) == 0;
 }
 ExpertGemmShape expert_shape(const sida_expert_gemm_config *c)
 {
@@ -151,7 +152,7 @@ int sida_route_backward(const sida_route_config *c, const void *logits_dev, int6
 size_t sida_expert_sort_workspace_bytes(int32_t E, int32_t top_k, int32_t T)
 {
     if (!pairs_ok(E, top_k, T)) return 0;
-    return up((size_t)expert_sort_chunks((int64_t)T * top_k) * E * 4, 256);
+    return up((size_t)expert_sort_most((int64_t)T * top_k) * E * 4, 256);
 }
 
 int sida_expert_sort(int32_t E, int32_t top_k, const int32_t *ids_dev, const float *gates_dev, int32_t T, int32_t *offsets_dev,
@@ -228,8 +229,8 @@ int sida_expert_gemm_input(const sida_expert_gemm_config *c, const void *dy_dev,
 size_t sida_expert_gemm_weights_workspace_bytes(const sida_expert_gemm_config *c, int32_t M)
 {
     if (!expert_cfg_ok(c, M)) return 0;
-    const int chunk = expert_weights_chunk(M, c->groups, c->N, c->K);
-    return chunk ? up((size_t)expert_weights_parts(M, c->groups, chunk) * c->N * (c->K + 1) * 4, 256) : 0;
+    if (!expert_weights_chunk(M, c->groups, c->N, c->K)) return 0;
+    return up((size_t)(expert_weights_most(c->groups, c->N, c->K) + c->groups) * c->N * (c->K + 1) * 4, 256);
 }
 
 int sida_expert_gemm_weights(const sida_expert_gemm_config *c, const void *dy_dev, int64_t ld_dy, const void *x_dev, int64_t ldx, int32_t M,
@@ -237,7 +238,7 @@ int sida_expert_gemm_weights(const sida_expert_gemm_config *c, const void *dy_de
 {
     if (!expert_cfg_ok(c, M) || c->activation != SIDA_ACT_NONE) return SIDA_EINVAL;
     if (M > 0 && (!matrix_ok(dy_dev, ld_dy, c->N, SIDA_BF16) || !matrix_ok(x_dev, ldx, c->K, SIDA_BF16))) return SIDA_EINVAL;
-    if (!dw_dev || !aligned(dw_dev, 16) || !aligned(d_bias_dev, 4) || !aligned(offsets_dev, 4) || (!offsets_dev && c->groups != 1) || !aligned(workspace_dev, 16))
+    if (!dw_dev || !aligned(dw_dev, 16) || !aligned(d_bias_dev, 16) || !aligned(offsets_dev, 4) || (!offsets_dev && c->groups != 1) || !aligned(workspace_dev, 16))
         return SIDA_EINVAL;
     const size_t need = sida_expert_gemm_weights_workspace_bytes(c, M);
     if (need && !workspace_dev) return SIDA_EINVAL;

@@ -87,7 +87,7 @@ __device__ __forceinline__ int anew(int v)
     return v;
 }
 // A descriptor's records, and a lane offset past them: such a load asks for nothing and brings zeros.  256 rows are at most
-// kMostExpertPitch values apart, so that every offset that is meant lies below.
+// kMostExpertPitch bytes apart, so that every offset that is meant lies below.
 constexpr uint32_t kRecords = 0x80000000u, kNowhere = 0xffffff00u;
 
 // ---- which tiles a workgroup takes --------------------------------------------------------------
@@ -871,13 +871,13 @@ __global__ __launch_bounds__(kFewWaves * 64) void expert_gemm_few(const GemmArgs
     write8(make_rsrc(g.out + ((int64_t)i0 * g.ldo + j0) * size, kRecords), r * (uint32_t)g.ldo + j, g.out32, f);
 }
 
-// The parts of each group's gradient, added in their order; 0 for a group without rows.  Eight values to a thread; what lies behind a matrix's last are the
-// biases.
-constexpr int kAddThreads = 256;
+// The parts of each group's gradient, added in their order; 0 for a group without rows.  Four values to a thread, eight parts asked for at a time; what lies
+// behind a matrix's last values are the biases.
+constexpr int kAddThreads = 256, kAddAhead = 8;
 __global__ __launch_bounds__(kAddThreads) void expert_weights_add(const GemmArgs g, const float *parts, const float *bias_parts)
 {
     const RowTiles rows(g, g.chunk);
-    const int64_t pieces = (int64_t)g.N * g.K / 8, all = pieces + (g.d_bias ? g.N / 8 : 0);
+    const int64_t pieces = (int64_t)g.N * g.K / 4, all = pieces + (g.d_bias ? g.N / 4 : 0);
     const int64_t blocks = (all + kAddThreads - 1) / kAddThreads;
     const int group = (int)(blockIdx.x / blocks);
     const int64_t p = blockIdx.x % blocks * kAddThreads + threadIdx.x;
@@ -885,25 +885,28 @@ __global__ __launch_bounds__(kAddThreads) void expert_weights_add(const GemmArgs
     rows.of(group, first, n);
     if (p >= all) return;
     const bool is_bias = p >= pieces;
-    const int64_t step = is_bias ? g.N : (int64_t)g.N * g.K, at = (is_bias ? p - pieces : p) * 8;
+    const int64_t step = is_bias ? g.N : (int64_t)g.N * g.K, at = (is_bias ? p - pieces : p) * 4;
     const float *from = (is_bias ? bias_parts : parts) + first * step + at;
-    F8 f{};
-    for (int c = 0; c < n; c += 4) {
-        f32x4 v[4][2];
+    f32x4 sum = {0, 0, 0, 0};
+    for (int c = 0; c < n; c += kAddAhead) {
+        f32x4 v[kAddAhead];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < n) {
-                v[i][0] = *reinterpret_cast<const f32x4 *>(from + (c + i) * step);
-                v[i][1] = *reinterpret_cast<const f32x4 *>(from + (c + i) * step + 4);
-            }
+        for (int i = 0; i < kAddAhead; ++i) v[i] = *reinterpret_cast<const f32x4 *>(from + min(c + i, n - 1) * step);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f.v[e] += v[i][0][e], f.v[4 + e] += v[i][1][e];
+        for (int i = 0; i < kAddAhead; ++i)
+            if (c + i < n) sum += v[i];
     }
-    if (is_bias) write8(make_rsrc(g.d_bias + (int64_t)group * g.N, kRecords), (uint32_t)at, true, f);
-    else write8(make_rsrc(g.out + (group * g.out_group + at) * (g.out32 ? 4 : 2), kRecords), 0, g.out32, f);
+    if (is_bias) {
+        *reinterpret_cast<f32x4 *>(g.d_bias + (int64_t)group * g.N + at) = sum;
+    } else if (g.out32) {
+        *reinterpret_cast<f32x4 *>(g.out + (group * g.out_group + at) * 4) = sum;
+    } else {
+        typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+        bf16x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (__bf16)sum[e];
+        *reinterpret_cast<bf16x4 *>(g.out + (group * g.out_group + at) * 2) = x;
+    }
 }
 
 template <Job JOB, int WI, int WJ, int MI, int NJ, int SA, int SB, int KB>
@@ -1000,7 +1003,7 @@ int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t
     p.d_bias = d_bias ? (float *)ws + expert_weights_parts(M, s.groups, g.chunk) * s.N * s.K : nullptr;
     const int e = launch_shape<Job::parts, 2, 2, 2, 2, 2, 3, 64>(p, st);
     if (e) return e;
-    const int64_t pieces = (int64_t)s.N * s.K / 8 + (d_bias ? s.N / 8 : 0);
+    const int64_t pieces = (int64_t)s.N * s.K / 4 + (d_bias ? s.N / 4 : 0);
     expert_weights_add<<<(uint32_t)(s.groups * ((pieces + kAddThreads - 1) / kAddThreads)), kAddThreads, 0, st>>>(g, (const float *)ws, p.d_bias);
     return (int)hipGetLastError();
 }

@@ -93,7 +93,7 @@ GEMM = [dict(cfg=False), dict(groups=0), dict(groups=257), dict(N=0), dict(N=60)
 
 
 @pytest.mark.parametrize("bad", GEMM + [dict(M=1 << 24, N=4096, ldy=4096), dict(x=0), dict(x=P + 8), dict(ldx=64), dict(ldx=76), dict(ldx=(1 << 22) + 8), dict(w=0), dict(w=P + 8),
-                                        dict(y=0), dict(y=P + 8), dict(ldy=56), dict(ldy=68), dict(ldy=66, out=sm.FP32), dict(ldy=(1 << 22) + 8), dict(bias=P + 4),
+                                        dict(y=0), dict(y=P + 8), dict(ldy=56), dict(ldy=68), dict(ldy=66, out=sm.FP32), dict(ldy=(1 << 21) + 4, out=sm.FP32), dict(ldy=1 << 62), dict(ldy=(1 << 22) + 8), dict(bias=P + 4),
                                         dict(pre=P + 8), dict(pre=2 * P, ld_pre=56), dict(res=P + 8), dict(res=2 * P, ld_res=56), dict(res=P, ld_res=72)])
 def test_gemm_refuses(bad):
     assert gemm(**bad) == EINVAL
@@ -109,6 +109,23 @@ def test_gemm_input_refuses(bad):
                                              dict(x=P + 8), dict(ldx=64), dict(dw=0), dict(dw=P + 8), dict(db=P + 2), dict(ws=P + 8)])
 def test_gemm_weights_refuses(bad):
     assert gemm_weights(**bad) == EINVAL
+
+
+def test_gemm_weights_workspace():
+    """Many rows into small matrices are summed in parts; what is enough for them is enough for fewer."""
+    for groups, N, K in ((4, 520, 264), (1, 1024, 1024), (1, 8, 8), (3, 128, 512)):
+        cfg, before = sm.SidaExpertGemmConfig(groups, N, K, sm.FP32, 0), 0
+        for M in (0, 1, 100, 512, 1000, 4097, 16385, 70000, 1 << 20):
+            n = sm.expert_gemm_weights_workspace_bytes(cfg, M)
+            assert n >= before
+            before = n
+            if n:
+                call = dict(groups=groups, N=N, K=K, M=M, ld_dy=N, ldx=K, out=sm.FP32)
+                assert gemm_weights(**call, n=n - 1) == ENOSPC and gemm_weights(**call, ws=0) == EINVAL
+        assert before
+    assert sm.expert_gemm_weights_workspace_bytes(sm.SidaExpertGemmConfig(64, 4096, 1024, sm.BF16, 0), 1 << 20) == 0
+    assert sm.expert_gemm_weights_workspace_bytes(sm.SidaExpertGemmConfig(4, 521, 264, sm.BF16, 0), 5) == 0
+    assert sm.expert_gemm_weights_workspace_bytes(sm.SidaExpertGemmConfig(4, 520, 264, sm.BF16, 0), -1) == 0
 
 
 def test_gemm_of_nothing():
