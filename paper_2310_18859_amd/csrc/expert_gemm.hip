@@ -450,7 +450,16 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
         total = (int64_t)rows.total * col_tiles * (JOB == Job::parts ? tiles_i : 1);
     }
     Items items(total, gridDim.x, 64);
-    auto next = [&](Work &w) {
+    // Zeros for a tile of a group without rows: no stages are spent on it.
+    auto clear = [&](const Work &w) {
+        const int of = g.out32 ? 4 : 8, pieces = w.rows_b / of;
+        char *to = g.out + (w.to * g.out_group + (int64_t)w.i0 * g.ldo + w.j0) * (g.out32 ? 4 : 2);
+        for (int p = tid; p < w.rows_a * pieces; p += Sh::kThreads)
+            *reinterpret_cast<i32x4 *>(to + ((int64_t)(p / pieces) * g.ldo + p % pieces * of) * (g.out32 ? 4 : 2)) = i32x4{0, 0, 0, 0};
+        if (g.d_bias && w.j0 == 0)
+            for (int i = tid; i < w.rows_a; i += Sh::kThreads) g.d_bias[(int64_t)w.to * g.N + w.i0 + i] = 0.f;
+    };
+    auto next_item = [&](Work &w) {
         const int id = items.next();
         if (id < 0) return false;
         if constexpr (kWeights) {
@@ -477,6 +486,13 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
         w.rows_b = min(Sh::BN, cols - w.j0);
         w = Work{uniform(w.a), uniform(w.b), uniform(w.rows_a), uniform(w.rows_b), uniform(w.c), uniform(w.i0), uniform(w.j0), uniform(w.group), uniform(w.to)};
         return true;
+    };
+    auto next = [&](Work &w) {
+        while (true) {
+            if (!next_item(w)) return false;
+            if (JOB != Job::weights || w.c > 0) return true;
+            clear(w);
+        }
     };
     auto stages_of = [&](const Work &w) { return max(Sh::kMost, (w.c + KB - 1) / KB); };
 
@@ -660,15 +676,14 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
             const int i = row_of(m, half), j = col0 + n * 32;
             return i < w.rows_a && j < w.rows_b ? i * (uint32_t)ld + j : kNone;
         };
-        // Beside the result is read: the bias of the tile's columns, and for each row `pre` (input, a block of rows ahead) or the residual (what an
-        // fp32 one has more than 16 bytes of, where it is used).
+        // Beside the result is read: the bias of the tile's columns, and for each row `pre` (input, a block of rows ahead) or the residual.
         F8 bias[NJ];
         if (JOB == Job::product && has_bias) {
 #pragma unroll
             for (int n = 0; n < NJ; ++n) bias[n] = read8(rb, col0 + n * 32 < w.rows_b ? (uint32_t)(col0 + n * 32) : kNone, true);
         }
         constexpr int kAhead = JOB == Job::input ? 1 : 0;     // blocks of rows (a product's bias has the registers of a second one)
-        i32x4 beside[kAhead + 1][NJ * 2];
+        i32x4 beside[kAhead + 1][NJ * 2], beside_high[JOB == Job::product ? NJ * 2 : 1];
         const int reads = JOB == Job::input ? has_pre : has_residual;
         auto ask = [&](int m) {
             if (kWeights || !reads) return;
@@ -680,6 +695,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
                 } else {
                     const uint32_t at = place(m, p / 2, p % 2, g.ld_res);
                     beside[m & kAhead][p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, (int)(at == kNone ? kNowhere : at * size), 0, 0));
+                    if (g.out32) beside_high[p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, (int)(at == kNone ? kNowhere : at * 4), 16, 0));
                 }
             }
         };
@@ -725,9 +741,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
                             const i32x4 low = beside[m & kAhead][n * 2 + h];
                             F8 s = widen(__builtin_bit_cast(bf16x8, low));
                             if (out32) {
-                                const uint32_t at = place(m, n, h, g.ld_res);
-                                const f32x4 a = __builtin_bit_cast(f32x4, low);
-                                const f32x4 b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, (int)(at == kNone ? kNowhere : at * 4), 16, 0));
+                                const f32x4 a = __builtin_bit_cast(f32x4, low), b = __builtin_bit_cast(f32x4, beside_high[n * 2 + h]);
                                 s = F8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
                             }
 #pragma unroll
