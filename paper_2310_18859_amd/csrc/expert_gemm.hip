@@ -50,16 +50,16 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, ui
 }
 // 16 bytes a lane straight into LDS: lane i's land at dst + 16 i.  Written out, because the compiler waits for all that it knows to be on its way to LDS
 // in front of each transposing read (8192 cubed, the input's gradient: 1089 us against 947); it has no register as its result, and waits that the compiler
-// counts without it wait longer, never shorter.  The pause: M0 is not there at once; settle() is that for scalar registers written by vector instructions.
+// counts without it wait longer, never shorter.  The pause: M0, and scalar registers that a vector instruction wrote, are not there at once, and inside the
+// statement the compiler does not see to that.
 __device__ __forceinline__ i32x4 lds_source(const char *base, uint32_t bytes)
 {
     return i32x4{(int)(uint32_t)(uint64_t)base, (int)((uint64_t)base >> 32 & 0xffff), (int)bytes, 0x00020000};
 }
 __device__ __forceinline__ void load_to_lds(i32x4 source, uint32_t offset, uint32_t dst)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(offset), "s"(source) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(offset), "s"(source) : "memory", "m0");
 }
-__device__ __forceinline__ void settle(i32x4 &a, i32x4 &b) { asm volatile("s_nop 4" : "+s"(a), "+s"(b)); }
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
@@ -526,7 +526,6 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
     auto prepare = [&] {
         if (Sh::kLeadB) prepare_b(), prepare_a();
         else prepare_a(), prepare_b();
-        settle(ra.source, rb.source);
     };
     constexpr int kLoads = Sh::kLoadsA + Sh::kLoadsB;
     auto load = [&](int i) {                                  // the leading operand's behind the other's
@@ -550,13 +549,11 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
     }
     if constexpr (SA > S) {
         ra.prepare();
-        settle(ra.source, rb.source);
 #pragma unroll
         for (int i = 0; i < Sh::kLoadsA; ++i) ra.load(i);
     }
     if constexpr (SB > S) {
         rb.prepare();
-        settle(ra.source, rb.source);
 #pragma unroll
         for (int i = 0; i < Sh::kLoadsB; ++i) rb.load(i);
     }
@@ -819,9 +816,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void expert_gemm_few(const GemmArgs
     const uint32_t at = (uint32_t)uniform((int)(uintptr_t)(__attribute__((address_space(3))) char *)mine);
     auto load = [&](int s) {                                  // this wavefront's stage s; past the end it asks for nothing
         const int c0 = (s * kFewWaves + wave) * 64, there = max(0, min(64, length - c0));
-        i32x4 from_a = lds_source(a + (there ? c0 * 2 : 0), (uint32_t)uniform(there ? (int)kRecords : 0));
-        i32x4 from_b = lds_source(b + (there ? (kAcross ? c0 * (int64_t)pitch_b : c0 * 2) : 0), (uint32_t)uniform((int)(kAcross ? there * pitch_b : there ? kRecords : 0)));
-        settle(from_a, from_b);
+        const i32x4 from_a = lds_source(a + (there ? c0 * 2 : 0), (uint32_t)uniform(there ? (int)kRecords : 0));
+        const i32x4 from_b = lds_source(b + (there ? (kAcross ? c0 * (int64_t)pitch_b : c0 * 2) : 0), (uint32_t)uniform((int)(kAcross ? there * pitch_b : there ? kRecords : 0)));
         const uint32_t dst = at + s % kFewStages * kStage;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
