@@ -87,6 +87,15 @@ def test_parts_fit_their_workspace(rule):
     assert cut > 100
 
 
+@pytest.mark.parametrize("groups,N,K", [(1, 8, 8), (1, 128, 128), (1, 256, 128), (2, 128, 64), (16, 8, 128), (100, 64, 64)])
+def test_parts_fit_their_workspace_a_little_above_a_multiple(rule, groups, N, K):
+    """Rows that are a few more than an even share for each part: one part more than there are shares, if the share were rounded down."""
+    most = rule.most(groups, N, K) - groups
+    for share in (256, 320, 4096):
+        for M in range(share * most, share * most + 600, 7):
+            assert rule.parts(M, groups, rule.chunk(M, groups, N, K)) <= most + groups
+
+
 def test_sorts_chunks(rule):
     for pairs in list(range(1, 9000, 61)) + [4096, 4097, 524288, 524289, 600000, 1 << 20, (1 << 26) - 1]:
         chunk, n = rule.sort_chunk(pairs), rule.sort_chunks(pairs)
