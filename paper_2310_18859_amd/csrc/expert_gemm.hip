@@ -23,7 +23,6 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
 
 enum class Job { product, input, weights, parts };           // parts: the weights' gradient of `chunk` rows at a time, to be added up
 
@@ -41,7 +40,7 @@ struct GemmArgs {
     const char *residual;
     int64_t ld_pre, ld_res;
     float *d_bias;               // weights
-    int chunk;                   // parts: rows of a part
+    int chunk, parts;            // parts: rows of a part, and parts at most, more than which only offsets that do not ascend would make
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *base, uint32_t bytes)
@@ -447,7 +446,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
         order = groups_by_rows<Sh::kThreads>(rows, g.groups, lds);
         total = (int64_t)g.groups * tiles_i * col_tiles;
     } else {
-        total = (int64_t)rows.total * col_tiles * (JOB == Job::parts ? tiles_i : 1);
+        total = (int64_t)(JOB == Job::parts ? min(rows.total, g.parts) * tiles_i : rows.total) * col_tiles;
     }
     Items items(total, gridDim.x, 64);
     // Zeros for a tile of a group without rows: no stages are spent on it.
@@ -665,7 +664,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
         const __amdgpu_buffer_rsrc_t ro = make_rsrc(g.out + ((kWeights ? w.to * g.out_group : 0) + (int64_t)w.i0 * g.ldo + w.j0) * size, kRecords);
         const __amdgpu_buffer_rsrc_t rp = make_rsrc(g.pre + ((int64_t)w.i0 * g.ld_pre + w.j0) * 2, kRecords);
         const __amdgpu_buffer_rsrc_t rr = make_rsrc(g.residual + ((int64_t)w.i0 * g.ld_res + w.j0) * size, kRecords);
-        const __amdgpu_buffer_rsrc_t rb = make_rsrc(g.bias + (JOB == Job::product ? (int64_t)w.group * g.N + w.j0 : 0), kRecords);
+        const __amdgpu_buffer_rsrc_t rbias = make_rsrc(g.bias + (JOB == Job::product ? (int64_t)w.group * g.N + w.j0 : 0), kRecords);
         const int l = anew(lane), quarter = l >> 4;
         const int col0 = wj * NJ * 32 + (quarter & 1) * 16 + (quarter >> 1) * 8;              // of block n: + 32 n
         auto row_of = [&](int m, int half) { return (m * WI + wi) * 32 + half * 16 + (l & 15); };
@@ -677,7 +676,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
         F8 bias[NJ];
         if (JOB == Job::product && has_bias) {
 #pragma unroll
-            for (int n = 0; n < NJ; ++n) bias[n] = read8(rb, col0 + n * 32 < w.rows_b ? (uint32_t)(col0 + n * 32) : kNone, true);
+            for (int n = 0; n < NJ; ++n) bias[n] = read8(rbias, col0 + n * 32 < w.rows_b ? (uint32_t)(col0 + n * 32) : kNone, true);
         }
         constexpr int kAhead = JOB == Job::input ? 1 : 0;     // blocks of rows (a product's bias has the registers of a second one)
         i32x4 beside[kAhead + 1][NJ * 2], beside_high[JOB == Job::product ? NJ * 2 : 1];
@@ -893,6 +892,7 @@ __global__ __launch_bounds__(kAddThreads) void expert_weights_add(const GemmArgs
     const int64_t p = blockIdx.x % blocks * kAddThreads + threadIdx.x;
     int first, n;
     rows.of(group, first, n);
+    n = min(n, g.parts - first);
     if (p >= all) return;
     const bool is_bias = p >= pieces;
     const int64_t step = is_bias ? g.N : (int64_t)g.N * g.K, at = (is_bias ? p - pieces : p) * 4;
@@ -929,7 +929,7 @@ int launch_shape(const GemmArgs &g, hipStream_t st)
     if (e) return e;
     int64_t tiles;                                            // at most
     if (Sh::kAcrossA) {
-        const int64_t matrices = JOB == Job::parts ? g.M / g.chunk + (g.groups < g.M ? g.groups : g.M) : g.groups;
+        const int64_t matrices = JOB == Job::parts ? g.parts : g.groups;
         tiles = matrices * ((g.N + Sh::BM - 1) / Sh::BM) * ((g.K + Sh::BN - 1) / Sh::BN);
     } else {
         const int cols = JOB == Job::product ? g.N : g.K;
@@ -1008,9 +1008,10 @@ int launch_expert_gemm_weights(const ExpertGemmShape &s, const void *dy, int64_t
         if (expert_weights_small(s.groups, s.N, s.K)) return launch_shape<Job::weights, 2, 2, 2, 2, 2, 3, 64>(g, st);
         return launch_shape<Job::weights, 2, 4, 4, 2, 2, 3, 64>(g, st);
     }
+    g.parts = (int)expert_weights_parts(M, s.groups, g.chunk);
     GemmArgs p = g;                                           // the parts, in fp32, behind one another; then their sums of dy
     p.out = (char *)ws, p.out32 = 1;
-    p.d_bias = d_bias ? (float *)ws + expert_weights_parts(M, s.groups, g.chunk) * s.N * s.K : nullptr;
+    p.d_bias = d_bias ? (float *)ws + (int64_t)g.parts * s.N * s.K : nullptr;
     const int e = launch_shape<Job::parts, 2, 2, 2, 2, 2, 3, 64>(p, st);
     if (e) return e;
     const int64_t pieces = (int64_t)s.N * s.K / 4 + (d_bias ? s.N / 4 : 0);

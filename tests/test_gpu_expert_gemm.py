@@ -231,6 +231,23 @@ def test_offsets_outside_are_clamped():
     assert y.eq(7).all()
 
 
+def test_offsets_that_do_not_ascend_stay_inside():
+    """Twice as many parts as ascending offsets could make: nothing behind the workspace, the gradients and the rows is written."""
+    M, groups, N, K = 16385, 4, 520, 264
+    dy, x = (t.to(BF).cuda() for t in inputs(10, (M, N), (M, K)))
+    at = torch.tensor([0, M, 0, M, 0], dtype=torch.int32, device="cuda")
+    need = sm.expert_gemm_weights_workspace_bytes(sm.SidaExpertGemmConfig(groups, N, K, sm.FP32, 0), M)
+    assert need
+    ws = torch.full((3 * need,), 7, dtype=torch.uint8, device="cuda")
+    dw, db = (torch.full((groups + 1,) + shape, 7.0, device="cuda") for shape in ((N, K), (N,)))
+    sm.expert_gemm_weights(dy, x, at, dw[:groups], ws[:need], stream(), d_bias=db[:groups])
+    assert ws[need:].eq(7).all() and dw[groups].eq(7).all() and db[groups].eq(7).all()
+    w = dw[:groups].to(BF)
+    y = torch.full((M + 9, N), 7.0, dtype=BF, device="cuda")
+    sm.expert_gemm(x, w, at, y[:M], stream())
+    assert y[M:].eq(7).all()
+
+
 def test_long_matrices():
     """Rows whose offsets in bytes and in values pass 32 bits."""
     M, N, K = 1100000, 2048, 64
