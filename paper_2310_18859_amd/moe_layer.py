@@ -24,6 +24,8 @@ class MoELayer:
     def __init__(self, E, d_model, d_ff, max_tokens, top_k=1, normalize=False, activation="gelu", device="cuda:0", stream=None):
         if activation not in ACTIVATIONS:
             raise ValueError(f"activation: one of {sorted(ACTIVATIONS)} is needed, not {activation!r}")
+        if d_model % 8 or d_ff % 8:
+            raise ValueError(f"d_model and d_ff: multiples of 8 are needed, not {d_model} and {d_ff}")
         self.dev = torch.device(device)
         if self.dev.type == "cuda" and self.dev.index is None:
             self.dev = torch.device("cuda", torch.cuda.current_device())
@@ -57,6 +59,8 @@ class MoELayer:
                                       (b_in, "b_in", (self.E, self.F), torch.float32), (b_out, "b_out", (self.E, self.d), torch.float32)):
             if t is not None or what[0] == "w":
                 self._need(t, what, shape, (dtype,))
+                if not t.is_contiguous():
+                    raise ValueError(f"{what}: a contiguous tensor is needed")
 
     def forward(self, x, logits, w_in, w_out, b_in=None, b_out=None, mask=None, residual=None):
         """x: bf16 [T, d_model]; logits: bf16 or fp32 [T, E]; mask: bool [T] or None; residual: bf16 [T, d_model] or None.  Returns y bf16 [T, d_model] and the
@@ -70,7 +74,7 @@ class MoELayer:
             self._need(residual, "residual", (T, self.d), (torch.bfloat16,))
         self._parameters(w_in, w_out, b_in, b_out)
         y, s = self._new(T, self.d), self.stream                           # memory of the caller's stream
-        pairs = T * self.k
+        pairs, self.tokens = T * self.k, None                              # a call that fails on its way leaves nothing to go back through
         with self._on_stream((self.ids, self.gates, self.counts, self.loss)):
             ids, gates, places = self.ids[:T], self.gates[:T], self.places[:T]
             route(logits, ids, gates, self.counts, self.loss, self.route_ws, s, mask=mask, normalize=self.normalize)
@@ -94,6 +98,8 @@ class MoELayer:
         self._need(dy, "dy", (T, self.d), (torch.bfloat16,))
         self._need(logits, "logits", (T, self.E))
         self._parameters(w_in, w_out, None, None)
+        if weights_dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"weights_dtype: {torch.float32} or {torch.bfloat16} is needed, not {weights_dtype}")
         out = {"dx": self._new(T, self.d), "d_logits": torch.empty_like(logits), "d_w_in": self._new(self.E, self.F, self.d, dtype=weights_dtype),
                "d_w_out": self._new(self.E, self.d, self.F, dtype=weights_dtype)}
         if biases:
