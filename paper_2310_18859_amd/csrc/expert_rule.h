@@ -5,7 +5,7 @@
 
 namespace sida {
 
-// ---- sort: pairs of a workgroup (a multiple of 1024), and workgroups; at most 256 of them up to 2^31 pairs
+// ---- sort: pairs of a workgroup (a multiple of 1024), and workgroups; at most 256 of them up to 2^31 pairs.  Up to 4096 pairs are one workgroup and one launch.
 constexpr int kExpertSortChunks = 256;
 inline int expert_sort_chunk(int64_t pairs)
 {
@@ -36,7 +36,19 @@ inline int rows_lanes_log2(int pieces)
 constexpr int64_t kMostExpertPitch = 1 << 23;
 
 // Which tiles the products of rows take, rows x columns: 32 x 32 with the sum shared by a workgroup's wavefronts, 32 x 128, 64 x 256, 128 x 128 (two
-// workgroups to a compute unit), 256 x 256 (one).
+// workgroups to a compute unit), 256 x 256 (one).  us for each, sizes as groups, mean rows of a group, length of the sum, columns:
+//     groups  rows  length  columns     few   32x128  64x256  128x128  256x256
+//          8   1/8    1024     4096     6.2     11.5    14.8     12.7     16.2
+//         64    17    1024     2048   137       61      64       60       83
+//         64    32    1024     4096   318      132     120      125      142
+//         64    64    4096     1024   254      155     137      159      222
+//         64   128    1024     4096   795      339     191      173      186
+//         64   256    1024     4096  1450      643     307      266      249
+//         64   512    4096     1024  2773     1249     598      503      405
+//          1  4096    1024     1024    79       27.5    22       21       37.5
+//          1  4096    1024     4096   329      130      54       54       45
+// `few`: as long as its tiles are one round of workgroups, more of them the longer the sum that is shared.  256 x 256 wants its tiles to fill the compute
+// units once at least, and four times where groups of fewer than 400 rows leave their last tile half empty.
 enum class ExpertTiles { few, rows32, rows64, square128, rows256 };
 inline ExpertTiles expert_tiles(int64_t M, int64_t groups, int64_t cols, int64_t length)
 {
@@ -49,7 +61,8 @@ inline ExpertTiles expert_tiles(int64_t M, int64_t groups, int64_t cols, int64_t
 }
 
 // ---- the weights' gradient: rows of a part (0: a group's rows are summed in one go).  Parts of 128 x 128 tiles where tiles of whole groups would leave
-// compute units idle, of as many rows as give each of the 512 workgroup slots one.
+// compute units idle, of as many rows as give each of the 512 workgroup slots one: with 384, 512, 768 and 1024 slots counted 4 experts of 520 x 264 and 16385
+// rows take 27.4, 28.5, 30.2 and 34.0 us (133 without parts), one of 1024 x 1024 and 4096 rows 32.5, 31.7, 35.7 and 43.8.
 inline int64_t expert_tiles_of(int64_t N, int64_t K, int64_t side) { return ((N + side - 1) / side) * ((K + side - 1) / side); }
 inline bool expert_weights_small(int64_t groups, int64_t N, int64_t K) { return groups * expert_tiles_of(N, K, 256) < 256; }
 inline int64_t expert_weights_most(int64_t groups, int64_t N, int64_t K) { return 512 / expert_tiles_of(N, K, 128) - groups / 2; }
