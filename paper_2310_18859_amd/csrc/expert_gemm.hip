@@ -7,9 +7,10 @@
 //
 // What bounds it, 32768 rows over 64 experts of 4096 x 1024 (Zipf 1.0), bf16: 2.7e11 operations are 196 us at 1.4 PFLOP/s, which a large library product
 // reaches here; bytes in and out are as many.  Measured: product with bias, GELU and the values in front of it kept 425 us, the input's gradient 420, the
-// weights' 449.  With 64 groups of 512 rows, without extras: 341, of which loads alone take 180 to 300 us (by how far the tiles' operands are in L2), the matrix
-// instructions 190, stores 80, and they overlap in part; LDS is read for 0.67 of the 1.8 us of a stage.  The compute clock is at 1.9 GHz then.  The library's batched
-// product of the same takes 319; one matrix of 32768 x 4096 x 1024 takes it 268, 269 and 392 us (product, input's, weights'), the kernels here 304, 244 and 305.
+// weights' 449.  With 64 groups of 512 rows, without extras: 320 to 341, of which loads alone take 180 to 300 us (by how far the tiles' operands are in L2), the matrix
+// instructions 190, stores 80, and they overlap in part; LDS is read for 0.67 of the 1.8 us of a stage.  The compute clock falls to 1.6 to 2.0 GHz then, by which the same cycles take
+// 10 % more or less time.  The library's batched product of the same takes 320; one matrix of 32768 x 4096 x 1024 takes it 259 to 268, 270 and 395 us (product,
+// input's, weights'), the kernels here 305, 239 and 300.
 #include <hip/hip_runtime.h>
 
 #include <cstddef>
@@ -106,7 +107,7 @@ struct Work {
 
 // The items that workgroup b takes one after the other, of `total`: b runs on XCD b % 8, and an XCD takes `block` items in a row of every eight
 // times as many, so that a row tile's rows and a group's matrix are fetched into few L2s while all XCDs get their share of large and small tiles.
-// 64 in a row are given, fewer where there are few items: from 8 to 4096 made no difference beyond that of two runs, nor did tiles in squares, or staggered starts.
+// 64 in a row are given, fewer where there are few items: from 8 to 4096 made no difference beyond that of two runs, nor did staggered starts.
 struct Items {
     int total, block, at, step;
     __device__ __forceinline__ Items(int64_t n, int workgroups, int most)
@@ -390,7 +391,7 @@ struct Shape {
 };
 
 // One operand's loads: a ring of S stages in LDS, and where the next stage comes from.  A lane's offsets are from where a stage begins in memory; along c its
-// first value of c says which loads a stage that is not whole leaves out, across c the descriptor ends with the last row.
+// first value of c says whether a stage that is not whole, the last one of a tile, has something for it; across c the descriptor ends with the last row.
 template <class T, bool ACROSS, int S, int KB, int WAVES>
 struct Ring {
     static constexpr int kLoads = T::kLoads / WAVES;
@@ -399,7 +400,7 @@ struct Ring {
     const char *from = nullptr;
     int left = 0, to_load = 0, slot = 0;                      // values of c, and stages, of the tile that are still to be asked for
     i32x4 source;
-    uint32_t dst, there;
+    uint32_t dst;
     __device__ __forceinline__ Ring(uint32_t lds, uint32_t pitch_, int wave) : lds_at(lds + wave * 1024), pitch(pitch_) {}
     __device__ __forceinline__ void begin(const char *tile, int rows, int length, int stages, int lane, int wave)
     {
@@ -410,7 +411,10 @@ struct Ring {
     __device__ __forceinline__ void end() { left = 0, to_load = INT32_MAX; }              // asks for nothing from now on
     __device__ __forceinline__ void prepare()
     {
-        there = left;
+        if (!ACROSS && (left & (KB - 1)) && left < KB) {      // the tile's last stage, and not a whole one (a comparison at each load instead: 2 to 3 %)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) off[i] = c < left ? off[i] : kNowhere;
+        }
         source = lds_source(from, (uint32_t)uniform((int)(ACROSS ? (uint32_t)min(left, KB) * pitch : left ? kRecords : 0)));
         dst = lds_at + slot * T::kBytes;
         left -= min(left, KB);
@@ -418,7 +422,7 @@ struct Ring {
         --to_load;
         slot = slot == S - 1 ? 0 : slot + 1;
     }
-    __device__ __forceinline__ void load(int i) { load_to_lds(source, ACROSS || c < (int)there ? off[i] : kNowhere, dst + i * WAVES * 1024); }
+    __device__ __forceinline__ void load(int i) { load_to_lds(source, off[i], dst + i * WAVES * 1024); }
 };
 
 template <int I>
@@ -492,8 +496,13 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
             w.rows_a = min(Sh::BM, g.N - w.i0);
         } else {
             w.to = 0;
-            rows.find(id / col_tiles, w.group, w.i0, w.rows_a);
-            w.j0 = id % col_tiles * Sh::BN;
+            // A matrix of its own (one group) is walked four rows of tiles at a time: an XCD's 32 tiles are 4 x 8 of them rather than 1 x 32, and L2 is asked for
+            // fewer lines that it has not got (8192 cubed: 1018 to 967 us; 32768 rows, 4096 x 1024, input's gradient: 300 to 293).  With 64 groups of
+            // a few rows of tiles each it makes no difference (415 and 416 us, Zipf 1.0).
+            const int together = g.groups == 1 ? 4 : 1, before = id / (together * col_tiles) * together, at = id - before * col_tiles;
+            const int tall = min(together, rows.total - before);
+            rows.find(before + at % tall, w.group, w.i0, w.rows_a);
+            w.j0 = at / tall * Sh::BN;
             w.a = g.a + (int64_t)w.i0 * g.lda * 2;
             w.b = g.b + (w.group * g.b_group + (JOB == Job::product ? w.j0 * g.ldb : (int64_t)w.j0)) * 2;
             w.c = JOB == Job::product ? g.K : g.N;

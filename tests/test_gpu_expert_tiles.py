@@ -16,6 +16,8 @@ SIZES = (
     + [("rows64", [41, 1, 0, 64, 65, 33, 96, 128] * 6, n, c) for n, c in ((520, 64), (648, 136), (1288, 8), (520, 776))]
     + [("square128", RAGGED + [128, 90, 129, 255, 256] * 3, n, c) for n, c in ((1032, 64), (1160, 200), (904, 520), (1288, 8), (2056, 328))]
     + [("rows256", [480 + 32 * i + (i * 7) % 32 for i in range(9)] * 3, n, c) for n, c in ((1800, 64), (2056, 200), (1544, 328), (1800, 136), (1544, 16))]
+    # one group, whose rows of tiles are walked four at a time, with one to three left over
+    + [("rows32", [300], 1600, 72), ("square128", [700], 4360, 136), ("square128", [590], 5640, 64), ("rows256", [4648], 3848, 72), ("rows256", [4200], 4104, 200)]
 )
 
 
