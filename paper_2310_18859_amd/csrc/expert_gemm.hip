@@ -6,8 +6,8 @@
 // the product) or with c across them (W in `input`, both operands in `weights`).
 //
 // What bounds it, 32768 rows over 64 experts of 4096 x 1024 (Zipf 1.0), bf16: 2.7e11 operations are 196 us at 1.4 PFLOP/s, which a large library product
-// reaches here; bytes in and out are as many.  Measured: product with bias, GELU and the values in front of it kept 425 us, the input's gradient 420, the
-// weights' 449.  With 64 groups of 512 rows, without extras: 320 to 341, of which loads alone take 180 to 300 us (by how far the tiles' operands are in L2), the matrix
+// reaches here; bytes in and out are as many.  Measured: product with bias, GELU and the values in front of it kept 414 to 432 us, the input's gradient 417 to
+// 448, the weights' 449 to 478, by the card.  With 64 groups of 512 rows, without extras: 320 to 341, of which loads alone take 180 to 300 us (by how far the tiles' operands are in L2), the matrix
 // instructions 190, stores 80, and they overlap in part; LDS is read for 0.67 of the 1.8 us of a stage.  The compute clock falls to 1.6 to 2.0 GHz then, by which the same cycles take
 // 10 % more or less time.  The library's batched product of the same takes 320; one matrix of 32768 x 4096 x 1024 takes it 259 to 268, 270 and 395 us (product,
 // input's, weights'), the kernels here 305, 239 and 300.
@@ -907,7 +907,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void expert_gemm_few(const GemmArgs
 }
 
 // The parts of each group's gradient, added in their order; 0 for a group without rows.  Four values to a thread, eight parts asked for at a time; what lies
-// behind a matrix's last values are the biases.  4 experts of 520 x 264 and 36 parts: 6.1 us, 20 MB and a launch.
+// behind a matrix's last values are the biases.  4 experts of 520 x 264 and 32 parts: 5.2 us, 20 MB and a launch.
 constexpr int kAddThreads = 256, kAddAhead = 8;
 __global__ __launch_bounds__(kAddThreads) void expert_weights_add(const GemmArgs g, const float *parts, const float *bias_parts)
 {
