@@ -105,27 +105,6 @@ struct Work {
     int group, to;               // to (weights): which of the result's matrices, the group's or the part's
 };
 
-// The items that workgroup b takes one after the other, of `total`: b runs on XCD b % 8, and an XCD takes `block` items in a row of every eight
-// times as many, so that a row tile's rows and a group's matrix are fetched into few L2s while all XCDs get their share of large and small tiles.
-// 64 in a row are given, fewer where there are few items: from 8 to 4096 made no difference beyond that of two runs, nor did staggered starts.
-struct Items {
-    int total, block, at, step;
-    __device__ __forceinline__ Items(int64_t n, int workgroups, int most)
-    {
-        const int rounds = (int)((n + workgroups - 1) / workgroups);
-        total = (int)n;
-        block = rounds ? min(most, (int)((n + 8 * rounds - 1) / (8 * rounds))) : 1;
-        at = blockIdx.x >> 3;
-        step = workgroups >> 3;
-    }
-    __device__ __forceinline__ int next()                     // -1: none
-    {
-        const int id = at / block * 8 * block + (blockIdx.x & 7) * block + at % block;
-        at += step;
-        return id < total ? id : -1;
-    }
-};
-
 // Where the groups begin, four of them to a lane.
 struct Groups {
     int at[5];
@@ -468,7 +447,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
     } else {
         total = (int64_t)(JOB == Job::parts ? min(rows.total, g.parts) * tiles_i : rows.total) * col_tiles;
     }
-    Items items(total, gridDim.x, 64);
+    Items items(total, gridDim.x, kItemsInARow, blockIdx.x);
     // Zeros for a tile of a group without rows: no stages are spent on it.
     auto clear = [&](const Work &w) {
         const int of = g.out32 ? 4 : 8, pieces = w.rows_b / of;
@@ -821,7 +800,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void expert_gemm_few(const GemmArgs
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int cols = JOB == Job::product ? g.N : g.K, col_tiles = (cols + 31) / 32, length = JOB == Job::product ? g.K : g.N;
     const RowTiles rows(g, 32);
-    Items items((int64_t)rows.total * col_tiles, gridDim.x, 64);
+    Items items((int64_t)rows.total * col_tiles, gridDim.x, kFewInARow, blockIdx.x);   // a workgroup takes one
     const int id = items.next();
     if (id < 0) return;
     int group, i0, n_rows;
@@ -974,8 +953,7 @@ int launch_few(const GemmArgs &g, hipStream_t st)
     const int e = allow_lds(grant, (const void *)expert_gemm_few<JOB>, kBytes);
     if (e) return e;
     const int cols = JOB == Job::product ? g.N : g.K;
-    const int64_t tiles = (int64_t)(g.M / 32 + (g.groups < g.M ? g.groups : g.M)) * ((cols + 31) / 32);
-    expert_gemm_few<JOB><<<(uint32_t)((tiles + 7) / 8 * 8), kFewWaves * 64, kBytes, st>>>(g);
+    expert_gemm_few<JOB><<<(uint32_t)expert_few_grid(g.M, g.groups, cols), kFewWaves * 64, kBytes, st>>>(g);
     return (int)hipGetLastError();
 }
 

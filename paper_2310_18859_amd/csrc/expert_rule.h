@@ -1,7 +1,13 @@
-// How the operators of plain bf16 experts cut up their work.  Plain code: the rules are checked without a GPU.
+// How the operators of plain bf16 experts cut up their work.  Plain code for host and device: the rules are checked without a GPU.
 #pragma once
 
 #include <cstdint>
+
+#if defined(__HIPCC__)
+#define SIDA_HD __host__ __device__ __forceinline__
+#else
+#define SIDA_HD inline
+#endif
 
 namespace sida {
 
@@ -59,6 +65,33 @@ inline ExpertTiles expert_tiles(int64_t M, int64_t groups, int64_t cols, int64_t
     if (mean <= 96) return ExpertTiles::rows64;
     return mean >= 256 && tiles(256, 256) >= (mean >= 400 ? 256 : 1024) ? ExpertTiles::rows256 : ExpertTiles::square128;
 }
+
+// Workgroups of `few`, one for each of the tiles that M rows in `groups` groups have at most, in eights.
+inline int64_t expert_few_grid(int64_t M, int64_t groups, int64_t cols)
+{
+    return ((M / 32 + (groups < M ? groups : M)) * ((cols + 31) / 32) + 7) / 8 * 8;
+}
+
+// The items that workgroup b of `workgroups` (a multiple of 8) takes one after the other, of n: b runs on XCD b % 8, and an XCD takes `block` items in a row of
+// every eight times as many, so that a row tile's rows and a group's matrix are fetched into few L2s while all XCDs get their share of large and small tiles.
+// kItemsInARow at most, fewer where there are few items: from 8 to 4096 made no difference beyond that of two runs, nor did staggered starts.
+// Workgroups that take one item only need an eighth of all items to an XCD: with shorter runs the last, incomplete eight of them are partly second items.
+constexpr int kItemsInARow = 64, kFewInARow = INT32_MAX;
+struct Items {
+    int total, block, xcd, at, step;
+    SIDA_HD Items(int64_t n, int workgroups, int most, int b) : total((int)n), xcd(b & 7), at(b >> 3), step(workgroups >> 3)
+    {
+        const int rounds = (int)((n + workgroups - 1) / workgroups);
+        const int64_t even = rounds ? (n + 8 * rounds - 1) / (8 * rounds) : 1;
+        block = (int)(most < even ? most : even);
+    }
+    SIDA_HD int next()                                        // -1: none
+    {
+        const int id = at / block * 8 * block + xcd * block + at % block;
+        at += step;
+        return id < total ? id : -1;
+    }
+};
 
 // ---- the weights' gradient: rows of a part (0: a group's rows are summed in one go).  Parts of 128 x 128 tiles where tiles of whole groups would leave
 // compute units idle, of as many rows as give each of the 512 workgroup slots one: with 384, 512, 768 and 1024 slots counted 4 experts of 520 x 264 and 16385
