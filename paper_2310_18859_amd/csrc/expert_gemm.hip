@@ -962,7 +962,7 @@ template <Job JOB>
 int launch_rows_job(const GemmArgs &g, hipStream_t st)
 {
     const int cols = JOB == Job::product ? g.N : g.K, length = JOB == Job::product ? g.K : g.N;
-    switch (expert_tiles(g.M, g.groups, cols, length)) {
+    switch (expert_tiles(g.M, g.groups, cols, length, JOB == Job::input)) {
     case ExpertTiles::few: return launch_few<JOB>(g, st);
     case ExpertTiles::rows32: return launch_shape<JOB, 1, 4, 1, 1, 4, 4, 64>(g, st);
     case ExpertTiles::rows64: return launch_shape<JOB, 1, 4, 2, 2, 2, 2, 64>(g, st);

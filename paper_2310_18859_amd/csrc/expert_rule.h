@@ -42,25 +42,39 @@ inline int rows_lanes_log2(int pieces)
 constexpr int64_t kMostExpertPitch = 1 << 23;
 
 // Which tiles the products of rows take, rows x columns: 32 x 32 with the sum shared by a workgroup's wavefronts, 32 x 128, 64 x 256, 128 x 128 (two
-// workgroups to a compute unit), 256 x 256 (one).  us for each, sizes as groups, mean rows of a group, length of the sum, columns:
-//     groups  rows  length  columns     few   32x128  64x256  128x128  256x256
-//          8   1/8    1024     4096     6.2     11.5    14.8     12.7     16.2
-//         64    17    1024     2048   137       61      64       60       83
-//         64    32    1024     4096   318      132     120      125      142
-//         64    64    4096     1024   254      155     137      159      222
-//         64   128    1024     4096   795      339     191      173      186
-//         64   256    1024     4096  1450      643     307      266      249
-//         64   512    4096     1024  2773     1249     598      503      405
-//          1  4096    1024     1024    79       27.5    22       21       37.5
-//          1  4096    1024     4096   329      130      54       54       45
-// `few`: as long as its tiles are one round of workgroups, more of them the longer the sum that is shared.  256 x 256 wants its tiles to fill the compute
-// units once at least, and four times where groups of fewer than 400 rows leave their last tile half empty.
+// workgroups to a compute unit), 256 x 256 (one).  us for each as product and as input's gradient, sizes as groups, rows of each (17: Zipf 1.2), length of
+// the sum, columns; one run on one card:
+//     groups  rows  length  columns       few        32x128      64x256     128x128     256x256
+//          8   1/8    1024     4096     8.5    7.5   12    11    15    15    13    12    16    15
+//         64    17    1024     2048   114    125     58    62    61    64    52    56    58    58
+//         64    32    1024     4096   222    259    102   115   104    97   106   111   107    98
+//         64    64    4096     1024   219    248    124   133   136   112   130   112   134    98
+//         64   128    1024     4096   665    729    289   323   144   138   129   135   134   121
+//         64   256    1024     4096  1269   1362    582   645   217   221   203   209   167   162
+//         64   512    4096     1024  1465   1626    672   788   384   382   311   315   260   258
+//          1  4096    1024     1024    74     80     27    25    20    20    18    18    31    30
+//          1  4096    1024     4096   289    318     87    83    47    48    44    43    39    39
+// `few`, a workgroup to a compute unit, against 32 x 128, by the number of its tiles that M and the groups allow.  Groups of one row each, weights out of memory:
+//     columns  length     256          384          512          640          768         1024         1280
+//        4096    1024    8.4  12.6   13.0  12.9   14.1  13.2   19.0  13.5   19.9  14.8   27.3  17.0   31.5  22.1      product
+//        4096    4096     16    31     27    33     36    37     40    42     43    49     64    63     68    77
+//        4096    8192     23    54     44    58     51    64     67    77     74    91     96   117    117   150
+//        4096    1024    9.0  12.0   14.6  12.8   16.1  13.4   20.4  14.4   21.8  15.7   28.8  18.9   33.3  23.5      input's gradient
+//        4096    4096     21    30     33    32     40    33     45    35     52    40     78    51     81    75
+//        4096    8192     28    50     57    57     76    60     80    64     94    75    141    96    145   145
+// Rows that fill half of their tiles or more make fewer of them than M and the groups allow (groups x rows, few and 32 x 128; length 4096, columns 1024 to 4096):
+//     product   8 x 16, 384 tiles: 17 and 31; 8 x 16, 768: 37 and 38; 1 x 128, 640: 28 and 31; 1 x 192, 896: 38 and 31
+//     input     8 x 16, 384 tiles: 24 and 34; 4 x 32, 512: 25 and 35; 1 x 128, 640: 36 and 31; 8 x 16, 768: 48 and 36
+// So the product takes `few` for more tiles the longer the sum, and the input's gradient, whose transposing reads take longer, for two rounds of workgroups at most.
+// 256 x 256 wants its tiles to fill the compute units once at least, and four times where groups of fewer than 400 rows leave
+// their last tile half empty.
 enum class ExpertTiles { few, rows32, rows64, square128, rows256 };
-inline ExpertTiles expert_tiles(int64_t M, int64_t groups, int64_t cols, int64_t length)
+inline ExpertTiles expert_tiles(int64_t M, int64_t groups, int64_t cols, int64_t length, bool input = false)
 {
     const int64_t active = groups < M ? groups : M, mean = M / groups;
     auto tiles = [&](int64_t rows, int64_t width) { return (M / rows + active) * ((cols + width - 1) / width); };
-    if (tiles(32, 32) <= 256 + length / 8) return ExpertTiles::few;
+    const int64_t most = 256 + length / 8;
+    if (tiles(32, 32) <= (input && most > 512 ? 512 : most)) return ExpertTiles::few;
     if (mean <= 24 || tiles(128, 128) <= 200) return ExpertTiles::rows32;
     if (mean <= 96) return ExpertTiles::rows64;
     return mean >= 256 && tiles(256, 256) >= (mean >= 400 ? 256 : 1024) ? ExpertTiles::rows256 : ExpertTiles::square128;

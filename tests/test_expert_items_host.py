@@ -34,6 +34,7 @@ extern "C" long grid(long M, long groups, long cols) { return expert_few_grid(M,
 extern "C" int most() { return kFewInARow; }
 extern "C" int walking_most() { return kItemsInARow; }
 extern "C" int pick(long M, long groups, long cols, long length) { return (int)expert_tiles(M, groups, cols, length); }
+extern "C" int pick_input(long M, long groups, long cols, long length) { return (int)expert_tiles(M, groups, cols, length, true); }
 """
 
 
@@ -47,7 +48,7 @@ def rule(tmp_path_factory):
     lib = ctypes.CDLL(so)
     lib.walk.argtypes = [ctypes.c_long, ctypes.c_int, ctypes.c_int, ctypes.c_int]
     lib.grid.argtypes, lib.grid.restype = [ctypes.c_long] * 3, ctypes.c_long
-    lib.pick.argtypes = [ctypes.c_long] * 4
+    lib.pick.argtypes = lib.pick_input.argtypes = [ctypes.c_long] * 4
     return lib
 
 
@@ -87,3 +88,13 @@ def test_sizes_of_the_gpu_tests(rule, counts, cols, length):
 def test_walking_workgroups(rule, workgroups):
     for n in list(range(1, 5000, 13)) + [511, 512, 513, 514, 4096, 16385, 65536, 1000003]:
         assert rule.walk(n, workgroups, rule.walking_most(), 0) == 0, n
+
+
+@pytest.mark.parametrize("M,cols,length,product,input_gradient", [
+    (2, 8192, 8192, "few", "few"), (1, 16416, 8192, "few", "rows32"), (5, 4096, 4096, "few", "rows32"), (6, 4096, 4096, "few", "rows32"), (7, 4096, 4096, "rows32", "rows32"),
+    (3, 4096, 1024, "few", "few"), (4, 4096, 1024, "rows32", "rows32"), (4, 4096, 2048, "few", "few"), (1, 8192, 8, "few", "few"), (1, 8448, 8, "rows32", "rows32"),
+])
+def test_lines_of_few_rows(rule, M, cols, length, product, input_gradient):
+    """As many tiles as the length of the sum allows, for the input's gradient no more than two rounds of workgroups."""
+    names = ("few", "rows32")
+    assert (names[rule.pick(M, 8, cols, length)], names[rule.pick_input(M, 8, cols, length)]) == (product, input_gradient)
