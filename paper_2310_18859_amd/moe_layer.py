@@ -54,24 +54,37 @@ class MoELayer:
         self.x_rows, self.y_rows = self._new(pairs, self.d), self._new(pairs, self.d)
         self.pre, self.h = self._new(pairs, self.F), self._new(pairs, self.F)
 
+    # What the library's calls refuse is refused here, before the first of them: the later ones would leave the buffers half overwritten.
+    def _matrix(self, t, what, shape, dtypes=(torch.bfloat16,)):
+        self._need(t, what, shape, dtypes)
+        rows, cols = shape
+        if t.numel() and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and not cols <= t.stride(0) < 1 << 24)):
+            raise ValueError(f"{what}: contiguous rows, one behind the other and less than 2^24 values apart, are needed, not strides {t.stride()}")
+
+    def _values(self, t, what, n, dtypes):
+        """At least n values one after the other, or None."""
+        if t is not None and (t.dtype not in dtypes or t.numel() < n or not t.is_contiguous() or t.device != self.dev):
+            raise ValueError(f"{what}: a contiguous tensor of at least {n} values of {' or '.join(str(d) for d in dtypes)} on {self.dev} is needed")
+
     def _parameters(self, w_in, w_out, b_in, b_out):
         for t, what, shape, dtype in ((w_in, "w_in", (self.E, self.F, self.d), torch.bfloat16), (w_out, "w_out", (self.E, self.d, self.F), torch.bfloat16),
                                       (b_in, "b_in", (self.E, self.F), torch.float32), (b_out, "b_out", (self.E, self.d), torch.float32)):
             if t is not None or what[0] == "w":
                 self._need(t, what, shape, (dtype,))
-                if not t.is_contiguous():
-                    raise ValueError(f"{what}: a contiguous tensor is needed")
+                if not t.is_contiguous() or t.data_ptr() % 16:
+                    raise ValueError(f"{what}: a contiguous tensor from a 16-byte boundary on is needed")
 
     def forward(self, x, logits, w_in, w_out, b_in=None, b_out=None, mask=None, residual=None):
         """x: bf16 [T, d_model]; logits: bf16 or fp32 [T, E]; mask: bool [T] or None; residual: bf16 [T, d_model] or None.  Returns y bf16 [T, d_model] and the
         balance loss [1]."""
         T = x.shape[0] if x.dim() else 0
-        self._need(x, "x", (T, self.d), (torch.bfloat16,))
+        self._matrix(x, "x", (T, self.d))
         if T > self.max_tokens:
             raise ValueError(f"x: at most {self.max_tokens} tokens, not {T}")
-        self._need(logits, "logits", (T, self.E))
+        self._matrix(logits, "logits", (T, self.E), (torch.bfloat16, torch.float32))
+        self._values(mask, "mask", T, (torch.bool, torch.uint8))
         if residual is not None:
-            self._need(residual, "residual", (T, self.d), (torch.bfloat16,))
+            self._matrix(residual, "residual", (T, self.d))
         self._parameters(w_in, w_out, b_in, b_out)
         y, s = self._new(T, self.d), self.stream                           # memory of the caller's stream
         pairs, self.tokens = T * self.k, None                              # a call that fails on its way leaves nothing to go back through
@@ -95,8 +108,10 @@ class MoELayer:
         T = self.tokens
         if T is None:
             raise RuntimeError("backward: there has been no forward call")
-        self._need(dy, "dy", (T, self.d), (torch.bfloat16,))
-        self._need(logits, "logits", (T, self.E))
+        self._matrix(dy, "dy", (T, self.d))
+        self._matrix(logits, "logits", (T, self.E), (torch.bfloat16, torch.float32))
+        self._values(mask, "mask", T, (torch.bool, torch.uint8))
+        self._values(d_loss, "d_loss", 1, (torch.float32,))
         self._parameters(w_in, w_out, None, None)
         if weights_dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"weights_dtype: {torch.float32} or {torch.bfloat16} is needed, not {weights_dtype}")
