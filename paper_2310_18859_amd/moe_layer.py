@@ -10,6 +10,7 @@ from .binding import (ACT_GELU, ACT_NONE, ACT_RELU, ACT_SILU, BF16, FP32, SidaEx
 from .mx_layer import MxMoELayer
 
 ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "silu": ACT_SILU}
+MOST_EXPERTS, MOST_TOP_K, MOST_WIDTH = 256, 8, 65536                       # of the library's calls, as are the limits of pairs in `forward`
 
 
 class MoELayer:
@@ -26,6 +27,9 @@ class MoELayer:
             raise ValueError(f"activation: one of {sorted(ACTIVATIONS)} is needed, not {activation!r}")
         if d_model % 8 or d_ff % 8:
             raise ValueError(f"d_model and d_ff: multiples of 8 are needed, not {d_model} and {d_ff}")
+        if not (1 <= E <= MOST_EXPERTS and 1 <= top_k <= min(E, MOST_TOP_K) and 8 <= d_model <= MOST_WIDTH and 8 <= d_ff <= MOST_WIDTH and
+                d_model * d_ff <= 1 << 30 and E * d_model * d_ff <= 1 << 36 and 0 <= max_tokens * top_k < 1 << 26):
+            raise ValueError(f"sizes that the experts' products take are needed, not {E} experts of {d_model} x {d_ff}, {top_k} to a token, {max_tokens} tokens")
         self.dev = torch.device(device)
         if self.dev.type == "cuda" and self.dev.index is None:
             self.dev = torch.device("cuda", torch.cuda.current_device())
@@ -81,6 +85,8 @@ class MoELayer:
         self._matrix(x, "x", (T, self.d))
         if T > self.max_tokens:
             raise ValueError(f"x: at most {self.max_tokens} tokens, not {T}")
+        if T * self.k > 1 << 24 or T * self.k * max(self.d, self.F) > 1 << 35:
+            raise ValueError(f"x: 2^24 pairs of token and expert and 2^35 values of their rows at most, not {T} tokens of {self.k} experts each")
         self._matrix(logits, "logits", (T, self.E), (torch.bfloat16, torch.float32))
         self._values(mask, "mask", T, (torch.bool, torch.uint8))
         if residual is not None:

@@ -1,4 +1,4 @@
-"""What the layer that can be trained refuses by strides, alignment and masks, before anything is enqueued and with the last call's way back still there: no GPU is
+"""What the layer that can be trained refuses by strides, alignment, masks and sizes, before anything is enqueued and with the last call's way back still there: no GPU is
 needed."""
 import contextlib
 
@@ -78,3 +78,22 @@ def test_backward(monkeypatch, bad):
 def test_backward_lets_through(monkeypatch, good):
     with pytest.raises(Reached):
         made(monkeypatch).backward(**{**BACK, **good})
+
+
+@pytest.mark.parametrize("k,d,F_,tokens", [(8, 8, 8, (1 << 21) + 1), (1, 8, 65536, (1 << 19) + 1), (1, 65536, 8, (1 << 19) + 1), (2, 4096, 16384, (1 << 20) + 1)])
+def test_more_pairs_than_the_products_take(monkeypatch, k, d, F_, tokens):
+    """Pairs up to 2^24, and pairs times width up to 2^35."""
+    layer = made(monkeypatch, k=k, d=d, F=F_, max_tokens=1 << 30)
+    for T, raised in ((tokens, ValueError), (tokens - 1, Reached)):
+        meta = dict(dtype=BF16, device="meta")
+        layer.dev, layer.tokens = torch.device("meta"), 5
+        with pytest.raises(raised):
+            layer.forward(torch.empty((T, d), **meta), torch.empty((T, E), **meta), torch.empty((E, F_, d), **meta), torch.empty((E, d, F_), **meta))
+        assert layer.tokens == (5 if raised is ValueError else None)
+
+
+@pytest.mark.parametrize("bad", [dict(E=0), dict(E=257), dict(top_k=0), dict(top_k=9, E=16), dict(top_k=5), dict(d_model=0), dict(d_ff=0), dict(d_model=65544),
+                                 dict(d_ff=65544), dict(d_model=32768, d_ff=32776), dict(E=256, d_model=16384, d_ff=16392), dict(max_tokens=-1), dict(max_tokens=1 << 25, top_k=2)])
+def test_sizes_refused(bad):
+    with pytest.raises(ValueError):
+        moe_layer.MoELayer(**{"E": E, "d_model": D, "d_ff": F, "max_tokens": 8, **bad})
