@@ -336,8 +336,8 @@ enum class RowsWay { out, sum, back };
 template <class V, int ALIGN>
 int launch_way(RowsArgs &a, RowsWay way, hipStream_t st)
 {
-    a.lanes_log2 = rows_lanes_log2(ALIGN >= 4 ? a.d * (int)sizeof(V) / 16 : a.d);
     const int64_t of = way == RowsWay::back ? (int64_t)a.T * a.k : a.T;
+    a.lanes_log2 = rows_lanes_log2(ALIGN >= 4 ? a.d * (int)sizeof(V) / 16 : a.d, of);
     const uint32_t grid = (uint32_t)(((of << a.lanes_log2) + kRowsThreads - 1) / kRowsThreads);
     auto by_pairs = [&](auto one, auto two, auto four, auto eight) {
         if (a.k == 1) one<<<grid, kRowsThreads, 0, st>>>(a);

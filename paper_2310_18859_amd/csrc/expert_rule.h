@@ -30,12 +30,12 @@ inline int expert_sort_chunks(int64_t pairs)
     return pairs <= c ? 1 : (int)((pairs + c - 1) / c);
 }
 
-// ---- rows: a token's lanes, 8 to 64
-inline int rows_lanes_log2(int pieces)
+// ---- rows: lanes of a token (or pair), 8 to 64; of more than 2^26 - 4 of them at most 32, as a launch has fewer than 2^32 threads in whole workgroups of 256
+inline int rows_lanes_log2(int pieces, int64_t tokens = 0)
 {
     int l = 3;
     while (l < 6 && 1 << l < pieces) ++l;
-    return l;
+    return l == 6 && tokens > (1 << 26) - 4 ? 5 : l;
 }
 
 // ---- products: bytes between two rows at most, so that 256 rows span less than 2^31
