@@ -7,10 +7,11 @@
 //
 // What bounds it, 32768 rows over 64 experts of 4096 x 1024 (Zipf 1.0), bf16: 2.7e11 operations are 196 us at 1.4 PFLOP/s, which a large library product
 // reaches here; bytes in and out are as many.  Measured: product with bias, GELU and the values in front of it kept 414 to 432 us, the input's gradient 417 to
-// 448, the weights' 449 to 478, by the card.  With 64 groups of 512 rows, without extras: 320 to 341, of which loads alone take 180 to 300 us (by how far the tiles' operands are in L2), the matrix
-// instructions 190, stores 80, and they overlap in part; LDS is read for 0.67 of the 1.8 us of a stage.  The compute clock falls to 1.6 to 2.0 GHz then, by which the same cycles take
-// 10 % more or less time.  The library's batched product of the same takes 320; one matrix of 32768 x 4096 x 1024 takes it 259 to 268, 270 and 395 us (product,
-// input's, weights'), the kernels here 305, 239 and 300.
+// 448, the weights' 449 to 478, by the card.  The matrix cores are busy 32, 31 and 26 % of the cycles (64 % of those of 8192 cubed): a workgroup has the compute unit
+// to itself, which multiplies nothing while a tile's results leave, so that bytes and products overlap in part only; the weights' gradient deals its tiles out
+// unevenly besides (groups_by_rows).  The compute clock falls to 1.6 to 2.0 GHz under them.  One card: 64 groups of 512 rows, without extras, 287, 260 and 355 us (product,
+// input's, weights' gradient), the library's batched product of the same 281; one matrix of 32768 x 4096 x 1024 takes the library 232, 221 and 321, the kernels
+// here 266, 235 and 302.
 #include <hip/hip_runtime.h>
 
 #include <cstddef>
@@ -183,8 +184,10 @@ struct RowTiles : Groups {
     }
 };
 
-// The groups by their number of rows, the largest first; the lower of equal ones: a tile's cost is its group's rows (weights), and the long ones must not come
-// last.  Four to a lane, a byte each.
+// The groups by their number of rows, the largest first; the lower of equal ones: a tile's cost is its group's rows (weights), and workgroups that take their last
+// tiles at about the same time are to have short ones then.  Four to a lane, a byte each.  It does not even out what they have altogether, as they take
+// tiles in fixed turns (Items): of 64 groups of 4096 x 1024 with 32768 rows (Zipf 1.0) the same two XCDs get the largest of every four, 198 stages a workgroup,
+// where the mean is 138 and the least 104 (449 to 478 us, by the card).  Even groups have 135 each (355 to 374 us).
 template <int THREADS>
 __device__ __forceinline__ uint32_t groups_by_rows(const Groups &groups, int n_groups, char *lds)
 {
@@ -415,10 +418,10 @@ struct Int {
 //
 // The shapes.  256 x 256 (eight wavefronts of 128 x 64; two stages of A, three of B, all of the 160 KiB): a value brought in goes into 256 products,
 // a fragment read from LDS into 2.7 matrix instructions on average, with 128 x 128 (four wavefronts of 64 x 64, two workgroups to a compute unit that cover each
-// other's results) into 128 and 2: 405 and 503 us for 64 groups of 512 rows, input's gradient of 4096 x 1024.  But it takes many tiles to fill 256 compute units
+// other's results) into 128 and 2: 258 and 315 us for 64 groups of 512 rows, input's gradient of 4096 x 1024.  But it takes many tiles to fill 256 compute units
 // evenly.  Wavefronts of 128 x 128 spill.
 // 32 x 128 and 64 x 256 are for groups of few rows, which are bound by bringing the experts' matrices in (1111 rows over 64 experts of 1024 x 2048, input's
-// gradient: 62 us for 45 of bytes).  The rule and its measurements: expert_rule.h.
+// gradient: 61 us at best for 45 of bytes).  The rule and its measurements: expert_rule.h.
 template <Job JOB, int WI, int WJ, int MI, int NJ, int SA, int SB, int KB>
 __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB>::kWaves * Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB>::kPerUnit / 4)) void expert_gemm_tiles(const GemmArgs g)
 {
@@ -785,7 +788,7 @@ __global__ __launch_bounds__(WI *WJ * 64, (Shape<JOB, WI, WJ, MI, NJ, SA, SB, KB
 
 // Few rows, few tiles: what counts is how long the way through the sum is.  A workgroup takes 32 rows and 32 columns, and its eight wavefronts share the
 // sum, 64 values of c at a time in turn, each with a ring of its own in LDS and no barrier; their parts meet in LDS and are added in a fixed order.
-// One row through an expert of 4096 x 1024: 6.3 us (32 x 128 tiles: 11.5; 8.4 MB, 1.4 us of bytes), the ways to memory of offsets, operands and bias after one another.
+// One row through an expert of 4096 x 1024: 6.2 us at best (a call 8.5, of 32 x 128 tiles 12.0; 8.4 MB, 1.4 us of bytes), the ways to memory of offsets, operands and bias after one another.
 constexpr int kFewWaves = 8, kFewStages = 2;
 template <Job JOB>
 __global__ __launch_bounds__(kFewWaves * 64) void expert_gemm_few(const GemmArgs g)

@@ -51,8 +51,8 @@ __global__ __launch_bounds__(kSortThreads) void expert_sort_count(const SortArgs
     if (tid < a.E) a.hist[(size_t)blockIdx.x * a.E + tid] = hist[tid];
 }
 
-// Bound by the way to memory and back, a few times over, as there are 256 KiB of pairs for 32768 tokens: 3.0 us for 128 pairs in one launch, 3.9 and 4.6 for
-// 65536 in two.  No second pass over floating-point or atomic places: a pair's place follows from the pairs in front of it, so that bits repeat.
+// Bound by the way to memory and back, a few times over, as there are 256 KiB of pairs for 32768 tokens: 3.0 us at best for 128 pairs in one launch, 3.8 and 4.6
+// for 65536 in two.  No second pass over floating-point or atomic places: a pair's place follows from the pairs in front of it, so that bits repeat.
 // A workgroup places the pairs of its chunk; each wavefront has a sixteenth of them, in order, 64 at a time.  A pair's place is the first
 // one of its expert, the expert's pairs in earlier chunks and wavefronts, in earlier turns of this one, and in lower lanes, which nine
 // ballots find.  ONE: there is one chunk, which counts for itself.
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kSortThreads) void expert_sort_place(const SortArgs
 
 // ---- rows ---------------------------------------------------------------------------------------
 // Bound by bytes where there are many tokens, and by the way to memory and back where there are few: what a token's pairs read is asked for together,
-// KM pairs and kDepth pieces of a row at a time.  32768 tokens of 1024 bf16 values, two experts each: out 28 us (182 MB with a tenth without a part, 6.5 TB/s, as L2
+// KM pairs and kDepth pieces of a row at a time.  32768 tokens of 1024 bf16 values, two experts each, at best: out 28 us (182 MB with a tenth without a part, 6.5 TB/s, as L2
 // and the cache behind it keep some), sum 45 us (256 MB, 5.7 TB/s), back 55 us (303 MB, 5.5 TB/s); a copy of a large matrix reaches 5.2.
 struct RowsArgs {
     const int32_t *places;

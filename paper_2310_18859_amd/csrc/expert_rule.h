@@ -88,7 +88,8 @@ inline int64_t expert_few_grid(int64_t M, int64_t groups, int64_t cols)
 
 // The items that workgroup b of `workgroups` (a multiple of 8) takes one after the other, of n: b runs on XCD b % 8, and an XCD takes `block` items in a row of
 // every eight times as many, so that a row tile's rows and a group's matrix are fetched into few L2s while all XCDs get their share of large and small tiles.
-// kItemsInARow at most, fewer where there are few items: from 8 to 4096 made no difference beyond that of two runs, nor did staggered starts.
+// kItemsInARow at most, fewer where there are few items: from 8 to 4096 made no difference beyond that of two runs, nor did staggered starts.  Nobody's turn depends on
+// what the items cost: where they are uneven, so are the workgroups' shares.
 // Workgroups that take one item only need an eighth of all items to an XCD: with shorter runs the last, incomplete eight of them are partly second items.
 constexpr int kItemsInARow = 64, kFewInARow = INT32_MAX;
 struct Items {
