@@ -1,5 +1,5 @@
 """Products of few rows whose tiles of 32 x 32 are more than an XCD's runs of 64 hold (512): every tile has to be somebody's.  Values are small whole numbers, so that
-products and sums are exact in fp32 and results the oracle's, to the bit; results hold another value first."""
+products and sums are exact in fp32 and results equal to the bit; results hold another value first."""
 import pytest
 import torch
 
